@@ -140,6 +140,64 @@ dq_status dq_mx_dar_hop(dq_codec fmt, const void *packed_in, const void *local, 
 dq_status dq_mx_decompress(dq_codec fmt, const void *packed_in, const void *local_or_null, dq_dtype dtype,
                            uint64_t n_entries, float *out, void *hip_stream);
 
+/* ---- 8-bit activation checkpoints, and the passes of a training step that write and read them: where the gradients that this
+ * library carries come from.  What the backward pass needs of the forward pass's activations waits in blocks of 32 entries along a
+ * row that share a power of two, as in the MXFP8 codec above.
+ *
+ * A checkpoint of rows x cols entries, pitch = cols rounded up to 32: rows * pitch E4M3 codes (the columns beyond cols are zero),
+ * then rows * pitch / 32 scale bytes, 16-byte aligned; the value of an entry is code * 2^(scale - 127).  With e = floor(log2 of the
+ * block's largest magnitude): scale = e + 127 - 8, but at least 10, so that every value is a normal bf16 number or zero (blocks
+ * below 2^-109 lose digits to that); codes round to nearest even and saturate at 448.  A block with an infinity or NaN has scale 255
+ * and reads as NaN throughout.  Where cols is a multiple of 32, these are dq_mx_compress's bytes for such tensors (of a multiple of
+ * 256 finite entries, blocks from 2^-109 on).
+ *
+ * The calls below take matrices: row r of `rows` at data + r * ld entries (ld >= cols where there are several rows; a part of a
+ * wider matrix is one), aligned to their entries, no more.  All matrices of a call have one type, except dw and what a load writes.
+ * What a call writes must not overlap anything else it is given (DQ_EINVAL); two matrices side by side in a wider one do not
+ * overlap.  rows or cols of zero: nothing is done, sums over no rows are zero.  Sums and statistics are binary32, in an order that
+ * the sizes and types fix: the same call gives the same bits.  Infinities and NaN go where the formulas take them. */
+typedef struct {
+  void *data; /* device; read-only operands are not written */
+  dq_dtype dtype;
+  uint64_t ld; /* entries from one row to the next; not looked at for a single row */
+} dq_matrix;
+typedef enum { DQ_SILU = 0, DQ_GELU = 1 } dq_activation; /* z / (1 + e^-z); z (1 + erf(z / sqrt 2)) / 2 */
+
+/* Bytes of a checkpoint (pure; 0 for no entries, or more than 2^46). */
+size_t dq_ckpt_bytes(uint64_t rows, uint64_t cols);
+dq_status dq_ckpt_save(const dq_matrix *x, uint64_t rows, uint64_t cols, void *ckpt, void *hip_stream);
+dq_status dq_ckpt_load(const void *ckpt, uint64_t rows, uint64_t cols, const dq_matrix *out, void *hip_stream);
+
+/* The weight gradient of a linear layer y = x w^T + b from the checkpoint of its input x (rows x cols) and dy (rows x outs):
+ *   dw[o][i] = sum over rows dy[.][o] x[.][i] (outs x cols),   db_or_null[o] = sum over rows dy[.][o] (of dw's type),
+ * added to what is there if `accumulate`: in binary32, then rounded once to dw's type.  scratch: device memory of
+ * dq_ckpt_weight_grad_scratch_bytes (of dy's type; may be 0, then NULL will do), 16-byte aligned, free again when the call's work
+ * is done.  rows, outs and cols below 2^31. */
+size_t dq_ckpt_weight_grad_scratch_bytes(dq_dtype dtype, uint64_t rows, uint64_t outs, uint64_t cols);
+dq_status dq_ckpt_weight_grad(const dq_matrix *dy, const void *ckpt, uint64_t rows, uint64_t outs, uint64_t cols, const dq_matrix *dw,
+                              void *db_or_null, int accumulate, void *scratch, size_t scratch_bytes, void *hip_stream);
+
+/* Layer norm along each row: y = (x - mean) rstd weight + bias, rstd = 1 / sqrt(mean of (x - mean)^2 + eps); weight and bias
+ * (cols entries of weight_dtype) may each be NULL.  For a backward pass ckpt, mean and rstd (one float a row) are given, all three:
+ * x goes to the checkpoint in the same pass; NULL all three otherwise.  cols below 2^31; eps finite, not negative. */
+dq_status dq_layer_norm(const dq_matrix *x, uint64_t rows, uint64_t cols, const void *weight, const void *bias, dq_dtype weight_dtype, float eps,
+                        const dq_matrix *y, void *ckpt, float *mean, float *rstd, void *hip_stream);
+/* Its backward pass, x read from the checkpoint: n = (x - mean) rstd, q = dy weight,
+ *   dx = rstd (q - avg(q) - n avg(q n)),   dweight = sum over rows dy n,   dbias = sum over rows dy
+ * (both of weight_dtype, added to what is there if `accumulate`; or both NULL). */
+size_t dq_layer_norm_grad_scratch_bytes(uint64_t rows, uint64_t cols);
+dq_status dq_layer_norm_grad(const dq_matrix *dy, const void *ckpt, const float *mean, const float *rstd, uint64_t rows, uint64_t cols,
+                             const void *weight, dq_dtype weight_dtype, const dq_matrix *dx, void *dweight, void *dbias, int accumulate, void *scratch,
+                             size_t scratch_bytes, void *hip_stream);
+
+/* The activation between two linear layers: h = act(z), or act(z) * u with a second input u (a gated block; NULL without).
+ * ckpt_z and ckpt_u (with u): the checkpoints that the backward pass reads, or NULL. */
+dq_status dq_gate(dq_activation kind, const dq_matrix *z, const dq_matrix *u, uint64_t rows, uint64_t cols, const dq_matrix *h, void *ckpt_z,
+                  void *ckpt_u, void *hip_stream);
+/* Its backward pass: dz = dh act'(z) [u], du = dh act(z) (ckpt_u and du both, or both NULL). */
+dq_status dq_gate_grad(dq_activation kind, const dq_matrix *dh, const void *ckpt_z, const void *ckpt_u, uint64_t rows, uint64_t cols,
+                       const dq_matrix *dz, const dq_matrix *du, void *hip_stream);
+
 /* ---- Hop replay (Section 3.4 "Reduce-scatter", Appendix B): N simulated workers whose
  * reordered gradients all live in this GPU's HBM; a transfer between workers is a pointer
  * hand-off.  Run step by step, one kernel launch per schedule step covers every (worker, chunk) job

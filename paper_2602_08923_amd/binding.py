@@ -8,6 +8,7 @@ schedules and whatever is set up once go through ctypes.
 """
 import ctypes as C
 import os
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -18,6 +19,7 @@ DQ_OK, DQ_EINVAL, DQ_EALIGN, DQ_EUNSUPPORTED, DQ_EHIP = range(5)
 DQ_F32, DQ_BF16 = 0, 1
 DQ_DYNAMIQ, DQ_MXFP8_E4M3, DQ_MXFP6_E3M2, DQ_MXFP4_E2M1 = 0, 1, 2, 3
 DQ_RING, DQ_BUTTERFLY, DQ_CHAIN = 0, 1, 2
+DQ_SILU, DQ_GELU = 0, 1
 
 EXPORTS = [
     "dq_create", "dq_destroy", "dq_set_round", "dq_packed_bytes", "dq_compress", "dq_dar_hop", "dq_decompress",
@@ -28,6 +30,8 @@ EXPORTS = [
     "dq_replay_destroy", "dq_status_str", "dq_last_hip_error",
     "dq_sg_stats", "dq_stats_combine", "dq_allocate", "dq_reorder", "dq_reorder_mean", "dq_restore",
     "dq_pipelined_wire_bytes", "dq_pipelined_stage_bytes", "dq_dar_hop_pipelined", "dq_dar_hop_pipelined_static",
+    "dq_ckpt_bytes", "dq_ckpt_save", "dq_ckpt_load", "dq_ckpt_weight_grad_scratch_bytes", "dq_ckpt_weight_grad",
+    "dq_layer_norm", "dq_layer_norm_grad_scratch_bytes", "dq_layer_norm_grad", "dq_gate", "dq_gate_grad",
 ]
 DQ_STATIC_STAGE_BYTES = 8 << 20
 
@@ -55,6 +59,11 @@ class ReplayDesc(C.Structure):
 class Local(C.Structure):
     """dq_local: a worker's own entries, their means, and where each super-group of the chunk lives."""
     _fields_ = [("data", C.c_void_p), ("dtype", C.c_int), ("mu", C.c_void_p), ("sg_index", C.c_void_p)]
+
+
+class Matrix(C.Structure):
+    """dq_matrix: rows of `ld` entries."""
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int), ("ld", C.c_uint64)]
 
 
 _lib = None
@@ -120,6 +129,19 @@ def lib():
         L.dq_pipelined_stage_bytes.restype = C.c_size_t
         L.dq_dar_hop_pipelined.argtypes = [vp, vp, C.POINTER(Local), C.POINTER(Chunk), u32, u32, vp, vp, vp, vp]
         L.dq_dar_hop_pipelined_static.argtypes = [vp, vp, C.POINTER(Local), C.POINTER(Chunk), u32, u32, vp, vp, vp]
+        m, sz = C.POINTER(Matrix), C.c_size_t
+        L.dq_ckpt_bytes.argtypes = [u64, u64]
+        L.dq_ckpt_save.argtypes = [m, u64, u64, vp, vp]
+        L.dq_ckpt_load.argtypes = [vp, u64, u64, m, vp]
+        L.dq_ckpt_weight_grad_scratch_bytes.argtypes = [i, u64, u64, u64]
+        L.dq_ckpt_weight_grad.argtypes = [m, vp, u64, u64, u64, m, vp, i, vp, sz, vp]
+        L.dq_layer_norm.argtypes = [m, u64, u64, vp, vp, i, C.c_float, m, vp, vp, vp, vp]
+        L.dq_layer_norm_grad_scratch_bytes.argtypes = [u64, u64]
+        L.dq_layer_norm_grad.argtypes = [m, vp, vp, vp, u64, u64, vp, i, m, vp, vp, i, vp, sz, vp]
+        L.dq_gate.argtypes = [i, m, m, u64, u64, m, vp, vp, vp]
+        L.dq_gate_grad.argtypes = [i, m, vp, vp, u64, u64, m, m, vp]
+        for f in (L.dq_ckpt_bytes, L.dq_ckpt_weight_grad_scratch_bytes, L.dq_layer_norm_grad_scratch_bytes):
+            f.restype = sz
         try:
             from . import _dqpy
         except ImportError as e:
@@ -248,6 +270,93 @@ def dq_mx_dar_hop(fmt, packed_in, local, packed_out=None):
 
 def dq_mx_decompress(fmt, packed_in, n_entries, local=None, out=None):
     return _native().mx_decompress(fmt, packed_in, n_entries, local, out)
+
+
+# ---- 8-bit activation checkpoints and the passes that write and read them ---------------
+# Tensors are of any number of dimensions: the last one's entries lie side by side, the others have one distance from row to row (a
+# part of a wider tensor is such a tensor; others take a .contiguous() first).  Calls run on the current stream of their tensors' device.
+
+class Checkpoint(NamedTuple):
+    """rows x cols activations in 8 bits: data (uint8, 16-byte aligned) holds dq_ckpt_bytes(rows, cols) bytes (include/dq.h has their order)."""
+    data: torch.Tensor
+    rows: int
+    cols: int
+
+
+class SavedNorm(NamedTuple):
+    """What a layer norm's forward pass leaves for its backward pass."""
+    x: Checkpoint
+    mean: torch.Tensor
+    rstd: torch.Tensor
+
+
+class SavedGate(NamedTuple):
+    """What an activation's forward pass leaves for its backward pass (u: None without a gate)."""
+    kind: str
+    z: Checkpoint
+    u: Optional[Checkpoint]
+
+
+_KINDS = {"silu": DQ_SILU, "gelu": DQ_GELU}
+
+
+def _kind(kind):
+    if kind not in _KINDS:
+        raise DqError(f"activations are {' and '.join(_KINDS)}")
+    return _KINDS[kind]
+
+
+def dq_ckpt_bytes(rows, cols):
+    return lib().dq_ckpt_bytes(rows, cols)
+
+
+def dq_ckpt_save(x, out=None):
+    """The checkpoint of x (float32 or bfloat16).  out: a uint8 tensor that takes its bytes."""
+    return Checkpoint(*_native().ckpt_save(x, out))
+
+
+def dq_ckpt_load(ckpt, dtype=torch.float32, out=None):
+    """A checkpoint's values, [rows, cols] (exact in either type)."""
+    return _native().ckpt_load(*ckpt, dtype is torch.bfloat16 or (None if dtype is not torch.float32 else False), out)
+
+
+def dq_ckpt_weight_grad(dy, ckpt, out=None, bias=False, bias_out=None, accumulate=False):
+    """dw = dy^T x, [outs, cols], of a linear layer whose input's checkpoint is ckpt, in dy's type or out's; with `bias` (or bias_out)
+    (dw, db), db = dy summed over its rows.  accumulate: added to out (and bias_out), which then have to be given."""
+    return _native().ckpt_weight_grad(dy, *ckpt, out, bool(bias), bias_out, bool(accumulate))
+
+
+def dq_layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, out=None):
+    """Layer norm over the last dimension; save: (y, SavedNorm), for dq_layer_norm_grad."""
+    got = _native().layer_norm(x, weight, bias, float(eps), bool(save), out)
+    if not save:
+        return got
+    y, data, rows, cols, mean, rstd = got
+    return y, SavedNorm(Checkpoint(data, rows, cols), mean, rstd)
+
+
+def dq_layer_norm_grad(dy, saved, weight=None, out=None, weight_out=None, bias_out=None, accumulate=False):
+    """(dx, dweight, dbias), the last two in weight's type, or None without a weight.  accumulate: added to weight_out and bias_out,
+    which then have to be given."""
+    x, mean, rstd = saved
+    return _native().layer_norm_grad(dy, *x, mean, rstd, weight, out, weight_out, bias_out, bool(accumulate))
+
+
+def dq_gate(z, u=None, kind="silu", save=False, out=None):
+    """act(z), or act(z) * u; kind: "silu" or "gelu" (by erf).  save: (h, SavedGate), for dq_gate_grad."""
+    got = _native().gate(_kind(kind), z, u, bool(save), out)
+    if not save:
+        return got
+    h, rows, cols, sz, su = got
+    return h, SavedGate(kind, Checkpoint(sz, rows, cols), None if su is None else Checkpoint(su, rows, cols))
+
+
+def dq_gate_grad(dh, saved, z_out=None, u_out=None):
+    """(dz, du), du None where there was no u."""
+    kind, z, u = saved
+    if u is not None and tuple(u[1:]) != tuple(z[1:]):
+        raise DqError("the checkpoints of z and u have one size")
+    return _native().gate_grad(_kind(kind), dh, *z, None if u is None else u[0], z_out, u_out)
 
 
 # ---- hop replay ------------------------------------------------------------------------

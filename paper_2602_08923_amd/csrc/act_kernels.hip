@@ -1,0 +1,306 @@
+// 8-bit activation checkpoints (save, load) and the activation between two linear layers, which saves its inputs as it reads them
+// and whose backward pass reads them from there.
+//
+// All are streams: every entry is read once and written once, a few dozen operations each, so memory bounds them.
+#include <atomic>
+#include <initializer_list>
+
+#include "act_rows.h"
+
+namespace dq {
+namespace {
+
+constexpr uint32_t kMapThreads = 256;
+
+// The chunks of a matrix, in order, dealt to the threads; rows that lie back to back are one long row (the host sees to it).
+struct Walk8 {
+  uint64_t chunks;             // in all
+  uint64_t per_row;            // of a row
+  uint64_t cols;
+  uint64_t step_rows, step_at; // a step of the whole grid, as rows and chunks
+};
+struct At {
+  uint64_t row, at, chunk;
+  __device__ __forceinline__ At(const Walk8 &w) {
+    chunk = (uint64_t)blockIdx.x * kMapThreads + threadIdx.x;
+    if (w.chunks >> 32) {
+      row = chunk / w.per_row;
+      at = chunk - row * w.per_row;
+    } else {
+      row = (uint32_t)chunk / (uint32_t)w.per_row;
+      at = (uint32_t)chunk - (uint32_t)row * (uint32_t)w.per_row;
+    }
+  }
+  __device__ __forceinline__ void next(const Walk8 &w) {
+    chunk += (uint64_t)gridDim.x * kMapThreads;
+    row += w.step_rows;
+    at += w.step_at;
+    if (at >= w.per_row) {
+      at -= w.per_row;
+      ++row;
+    }
+  }
+};
+template <typename T>
+__device__ __forceinline__ uint8_t *row_of(const Rows &m, uint64_t row) {
+  return static_cast<uint8_t *>(m.data) + row * m.ld * kEntry<T>;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kMapThreads) void k_ckpt_save(Walk8 w, Rows x, CkptOut out) {
+  for (At i(w); i.chunk < w.chunks; i.next(w)) {
+    float v[8];
+    load8<T>(row_of<T>(x, i.row), i.at * 8, w.cols, v);
+    ckpt_store8(out, i.chunk, v);
+  }
+}
+template <typename T>
+__global__ __launch_bounds__(kMapThreads) void k_ckpt_load(Walk8 w, CkptIn in, Rows x) {
+  for (At i(w); i.chunk < w.chunks; i.next(w)) {
+    float v[8];
+    ckpt_load8(in, i.chunk, v);
+    store8<T>(row_of<T>(x, i.row), i.at * 8, w.cols, v);
+  }
+}
+
+// a = act(z), d = act'(z).
+template <int KIND>
+__device__ __forceinline__ void activation(float z, float *a, float *d) {
+  if constexpr (KIND == DQ_SILU) {  // z p with p = 1 / (1 + e^-z); the derivative is p + z p (1 - p)
+    const float p = 1.0f / (1.0f + expf(-z));
+    *a = z * p;
+    *d = p * fmaf(z, 1.0f - p, 1.0f);
+  } else {  // z p with p = (1 + erf(z / sqrt 2)) / 2, the normal distribution; the derivative is p + z times its density
+    const float p = 0.5f * erfcf(-0.70710678118654752f * z);
+    *a = z * p;
+    *d = fmaf(z * 0.39894228040143268f, expf(-0.5f * z * z), p);
+  }
+}
+
+template <typename T, int KIND, bool GATED, bool SAVE>
+__global__ __launch_bounds__(kMapThreads) void k_gate(Walk8 w, Rows z, Rows u, Rows h, CkptOut sz, CkptOut su) {
+  for (At i(w); i.chunk < w.chunks; i.next(w)) {
+    float a[8], b[8], d;
+    load8<T>(row_of<T>(z, i.row), i.at * 8, w.cols, a);
+    if constexpr (GATED) load8<T>(row_of<T>(u, i.row), i.at * 8, w.cols, b);
+    if constexpr (SAVE) ckpt_store8(sz, i.chunk, a);
+    if constexpr (SAVE && GATED) ckpt_store8(su, i.chunk, b);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      activation<KIND>(a[k], &a[k], &d);
+      if constexpr (GATED) a[k] *= b[k];
+    }
+    store8<T>(row_of<T>(h, i.row), i.at * 8, w.cols, a);
+  }
+}
+template <typename T, int KIND, bool GATED>
+__global__ __launch_bounds__(kMapThreads) void k_gate_grad(Walk8 w, Rows dh, CkptIn sz, CkptIn su, Rows dz, Rows du) {
+  for (At i(w); i.chunk < w.chunks; i.next(w)) {
+    float g[8], a[8], b[8];
+    load8<T>(row_of<T>(dh, i.row), i.at * 8, w.cols, g);
+    ckpt_load8(sz, i.chunk, a);
+    if constexpr (GATED) ckpt_load8(su, i.chunk, b);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      float act, d;
+      activation<KIND>(a[k], &act, &d);
+      if constexpr (GATED) {
+        a[k] = g[k] * b[k] * d;
+        b[k] = g[k] * act;
+      } else {
+        a[k] = g[k] * d;
+      }
+    }
+    store8<T>(row_of<T>(dz, i.row), i.at * 8, w.cols, a);
+    if constexpr (GATED) store8<T>(row_of<T>(du, i.row), i.at * 8, w.cols, b);
+  }
+}
+
+struct Map {
+  Walk8 walk;
+  uint32_t blocks;
+};
+// Rows back to back without padding in any operand are walked as one long row.
+Map plan_map(uint64_t rows, uint64_t cols, std::initializer_list<const dq_matrix *> m) {
+  bool flat = cols % kCkptBlock == 0;
+  for (const dq_matrix *x : m) flat = flat && (rows == 1 || x->ld == cols);
+  if (flat) {
+    cols *= rows;
+    rows = 1;
+  }
+  Map p;
+  p.walk.per_row = ckpt_pitch(cols) / 8;
+  p.walk.chunks = rows * p.walk.per_row;
+  p.walk.cols = cols;
+  const uint64_t want = (p.walk.chunks + kMapThreads - 1) / kMapThreads, most = (uint64_t)device_cu_count() * 8;
+  p.blocks = (uint32_t)(want < most ? want : most);
+  const uint64_t step = (uint64_t)p.blocks * kMapThreads;
+  p.walk.step_rows = step / p.walk.per_row;
+  p.walk.step_at = step % p.walk.per_row;
+  return p;
+}
+Rows rows_of(const dq_matrix *m) { return m ? Rows{m->data, m->ld} : Rows{nullptr, 0}; }
+
+bool good_kind(dq_activation k) { return k == DQ_SILU || k == DQ_GELU; }
+bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+}  // namespace
+
+bool regions_meet(const Region *r, int n) {
+  for (int i = 0; i < n; ++i)
+    for (int j = i + 1; j < n; ++j) {
+      const Region &a = r[i], &b = r[j];
+      if (!a.p || !b.p || (!a.written && !b.written) || !a.rows || !b.rows || !a.bytes || !b.bytes) continue;
+      const uint64_t pa = (uint64_t)(uintptr_t)a.p, pb = (uint64_t)(uintptr_t)b.p;
+      if (pa + (a.rows - 1) * a.stride + a.bytes <= pb || pb + (b.rows - 1) * b.stride + b.bytes <= pa) continue;
+      if (a.rows > 1 && b.rows > 1 && a.stride == b.stride) {  // side by side in one wider matrix
+        const uint64_t off = pb >= pa ? (pb - pa) % a.stride : (a.stride - (pa - pb) % a.stride) % a.stride;
+        if (off >= a.bytes && off + b.bytes <= a.stride) continue;
+      }
+      return true;
+    }
+  return false;
+}
+
+dq_status check_matrix(const dq_matrix *m, uint64_t rows, uint64_t cols) {
+  if (!m || (m->dtype != DQ_F32 && m->dtype != DQ_BF16)) return DQ_EINVAL;
+  if (rows == 0 || cols == 0) return DQ_OK;
+  if (!m->data || (rows > 1 && m->ld < cols)) return DQ_EINVAL;
+  if ((uintptr_t)m->data % entry_bytes(m->dtype)) return DQ_EALIGN;
+  const uint64_t most = 1ull << 46;  // entries from the first to the last
+  if (cols > most || (rows > 1 && (m->ld > most || (rows - 1) > (most - cols) / m->ld))) return DQ_EUNSUPPORTED;
+  return DQ_OK;
+}
+
+// Asked once per device and kept (the number of CUs does not change).
+uint32_t device_cu_count() {
+  static std::atomic<uint32_t> known[64];
+  int device = 0;
+  if (hipGetDevice(&device) != hipSuccess || device < 0 || device >= 64) return 256;
+  uint32_t n = known[device].load(std::memory_order_relaxed);
+  if (n == 0) {
+    int cus = 0;
+    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess || cus <= 0) return 256;
+    known[device].store(n = (uint32_t)cus, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+}  // namespace dq
+
+using namespace dq;
+
+#define DQ_TRY(x)                     \
+  do {                                \
+    const dq_status st_ = (x);        \
+    if (st_ != DQ_OK) return st_;     \
+  } while (0)
+#define DQ_RUN(kernel, p, ...) \
+  hipLaunchKernelGGL((kernel), dim3((p).blocks), dim3(kMapThreads), 0, (hipStream_t)hip_stream, (p).walk, __VA_ARGS__)
+
+extern "C" {
+
+size_t dq_ckpt_bytes(uint64_t rows, uint64_t cols) {
+  if (rows == 0 || cols == 0 || cols > (1ull << 46) || rows > (1ull << 46) / ckpt_pitch(cols)) return 0;
+  const uint64_t codes = rows * ckpt_pitch(cols);
+  return (size_t)(codes + codes / kCkptBlock);
+}
+
+dq_status dq_ckpt_save(const dq_matrix *x, uint64_t rows, uint64_t cols, void *ckpt, void *hip_stream) {
+  DQ_TRY(check_matrix(x, rows, cols));
+  if (rows == 0 || cols == 0) return DQ_OK;
+  const size_t bytes = dq_ckpt_bytes(rows, cols);
+  if (bytes == 0) return DQ_EUNSUPPORTED;
+  if (!ckpt) return DQ_EINVAL;
+  if (!al16(ckpt)) return DQ_EALIGN;
+  const Region r[] = {region(x, rows, cols, false), region(ckpt, bytes, true)};
+  if (regions_meet(r, 2)) return DQ_EINVAL;
+  const Map p = plan_map(rows, cols, {x});
+  if (x->dtype == DQ_F32) DQ_RUN(k_ckpt_save<F32>, p, rows_of(x), ckpt_out(ckpt, rows, cols));
+  else DQ_RUN(k_ckpt_save<Bf16>, p, rows_of(x), ckpt_out(ckpt, rows, cols));
+  return hip_status(hipGetLastError());
+}
+
+dq_status dq_ckpt_load(const void *ckpt, uint64_t rows, uint64_t cols, const dq_matrix *out, void *hip_stream) {
+  DQ_TRY(check_matrix(out, rows, cols));
+  if (rows == 0 || cols == 0) return DQ_OK;
+  const size_t bytes = dq_ckpt_bytes(rows, cols);
+  if (bytes == 0) return DQ_EUNSUPPORTED;
+  if (!ckpt) return DQ_EINVAL;
+  if (!al16(ckpt)) return DQ_EALIGN;
+  const Region r[] = {region(ckpt, bytes, false), region(out, rows, cols, true)};
+  if (regions_meet(r, 2)) return DQ_EINVAL;
+  const Map p = plan_map(rows, cols, {out});
+  if (out->dtype == DQ_F32) DQ_RUN(k_ckpt_load<F32>, p, ckpt_in(ckpt, rows, cols), rows_of(out));
+  else DQ_RUN(k_ckpt_load<Bf16>, p, ckpt_in(ckpt, rows, cols), rows_of(out));
+  return hip_status(hipGetLastError());
+}
+
+dq_status dq_gate(dq_activation kind, const dq_matrix *z, const dq_matrix *u, uint64_t rows, uint64_t cols, const dq_matrix *h, void *ckpt_z,
+                  void *ckpt_u, void *hip_stream) {
+  if (!good_kind(kind)) return DQ_EINVAL;
+  DQ_TRY(check_matrix(z, rows, cols));
+  DQ_TRY(check_matrix(h, rows, cols));
+  if (u) DQ_TRY(check_matrix(u, rows, cols));
+  if (h->dtype != z->dtype || (u && u->dtype != z->dtype) || (u ? !ckpt_z != !ckpt_u : ckpt_u != nullptr)) return DQ_EINVAL;
+  if (rows == 0 || cols == 0) return DQ_OK;
+  const size_t bytes = dq_ckpt_bytes(rows, cols);
+  if (bytes == 0) return DQ_EUNSUPPORTED;
+  if (!al16(ckpt_z) || !al16(ckpt_u)) return DQ_EALIGN;
+  const Region r[] = {region(z, rows, cols, false), region(u ? u : z, rows, cols, false), region(h, rows, cols, true), region(ckpt_z, bytes, true),
+                      region(ckpt_u, bytes, true)};
+  if (regions_meet(r, 5)) return DQ_EINVAL;
+  const Map p = u ? plan_map(rows, cols, {z, u, h}) : plan_map(rows, cols, {z, h});
+  const Rows rz = rows_of(z), ru = rows_of(u), rh = rows_of(h);
+  const CkptOut sz = ckpt_out(ckpt_z, rows, cols), su = ckpt_out(ckpt_u, rows, cols);
+#define DQ_GATE(T, K)                                                                   \
+  do {                                                                                  \
+    if (u && ckpt_z) DQ_RUN((k_gate<T, K, true, true>), p, rz, ru, rh, sz, su);         \
+    else if (u) DQ_RUN((k_gate<T, K, true, false>), p, rz, ru, rh, sz, su);             \
+    else if (ckpt_z) DQ_RUN((k_gate<T, K, false, true>), p, rz, ru, rh, sz, su);        \
+    else DQ_RUN((k_gate<T, K, false, false>), p, rz, ru, rh, sz, su);                   \
+  } while (0)
+  if (z->dtype == DQ_F32) {
+    if (kind == DQ_SILU) DQ_GATE(F32, DQ_SILU);
+    else DQ_GATE(F32, DQ_GELU);
+  } else {
+    if (kind == DQ_SILU) DQ_GATE(Bf16, DQ_SILU);
+    else DQ_GATE(Bf16, DQ_GELU);
+  }
+  return hip_status(hipGetLastError());
+}
+
+dq_status dq_gate_grad(dq_activation kind, const dq_matrix *dh, const void *ckpt_z, const void *ckpt_u, uint64_t rows, uint64_t cols,
+                       const dq_matrix *dz, const dq_matrix *du, void *hip_stream) {
+  if (!good_kind(kind)) return DQ_EINVAL;
+  DQ_TRY(check_matrix(dh, rows, cols));
+  DQ_TRY(check_matrix(dz, rows, cols));
+  if (du) DQ_TRY(check_matrix(du, rows, cols));
+  if (dz->dtype != dh->dtype || (du && du->dtype != dh->dtype)) return DQ_EINVAL;
+  if (rows == 0 || cols == 0) return DQ_OK;
+  const size_t bytes = dq_ckpt_bytes(rows, cols);
+  if (bytes == 0) return DQ_EUNSUPPORTED;
+  if (!ckpt_z || !ckpt_u != !du) return DQ_EINVAL;
+  if (!al16(ckpt_z) || !al16(ckpt_u)) return DQ_EALIGN;
+  const Region r[] = {region(dh, rows, cols, false), region(ckpt_z, bytes, false), region(ckpt_u, bytes, false), region(dz, rows, cols, true),
+                      du ? region(du, rows, cols, true) : region(nullptr, 0, true)};
+  if (regions_meet(r, 5)) return DQ_EINVAL;
+  const Map p = du ? plan_map(rows, cols, {dh, dz, du}) : plan_map(rows, cols, {dh, dz});
+  const Rows rg = rows_of(dh), rz = rows_of(dz), ru = rows_of(du);
+  const CkptIn sz = ckpt_in(ckpt_z, rows, cols), su = ckpt_in(ckpt_u, rows, cols);
+#define DQ_GATE_GRAD(T, K)                                                        \
+  do {                                                                            \
+    if (du) DQ_RUN((k_gate_grad<T, K, true>), p, rg, sz, su, rz, ru);             \
+    else DQ_RUN((k_gate_grad<T, K, false>), p, rg, sz, su, rz, ru);               \
+  } while (0)
+  if (dh->dtype == DQ_F32) {
+    if (kind == DQ_SILU) DQ_GATE_GRAD(F32, DQ_SILU);
+    else DQ_GATE_GRAD(F32, DQ_GELU);
+  } else {
+    if (kind == DQ_SILU) DQ_GATE_GRAD(Bf16, DQ_SILU);
+    else DQ_GATE_GRAD(Bf16, DQ_GELU);
+  }
+  return hip_status(hipGetLastError());
+}
+
+}  // extern "C"

@@ -1,0 +1,182 @@
+// Rows of activations as the checkpoint, layer norm, gate and weight-gradient kernels read and write them, and the checkpoint's
+// 8-bit blocks.
+//
+// A row is cut into chunks of 8 entries, one lane's share; four neighbouring lanes hold a block of 32.  Rows start at any multiple
+// of the entry size: gfx950 loads and stores 16 bytes from any address, at full rate where they do not cross a cache line, so
+// there is one path for every stride, and only a row's last chunk may have to go entry by entry.
+#pragma once
+#include "dq_device.h"
+
+namespace dq {
+
+typedef uint32_t a32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t a32x4 __attribute__((ext_vector_type(4)));
+typedef float af32x4 __attribute__((ext_vector_type(4)));
+typedef float af32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef a32x4 a32x4_any __attribute__((aligned(2)));   // 16 bytes from any bf16's address
+typedef af32x4 af32x4_any __attribute__((aligned(4)));
+
+// rows x cols entries, row r from data + r * ld entries on
+struct Rows {
+  void *data;
+  uint64_t ld;
+};
+inline uint32_t entry_bytes(dq_dtype t) { return t == DQ_F32 ? 4u : 2u; }
+
+constexpr uint32_t kCkptBlock = 32;
+// Scale bytes: 10 is the least (8-bit values are then normal bf16 numbers or zero, whatever reads them), 246 is that of the
+// largest binary32; 255 marks a block with an infinity or NaN, all of whose codes are NaN.
+constexpr uint32_t kCkptLeast = 10;
+inline __host__ __device__ uint64_t ckpt_pitch(uint64_t cols) { return (cols + kCkptBlock - 1) / kCkptBlock * kCkptBlock; }
+
+template <typename T>
+__device__ __forceinline__ T a_ld(const void *p) {
+  return *(const __attribute__((address_space(1))) T *)p;
+}
+template <typename T>
+__device__ __forceinline__ void a_st(void *p, T v) {
+  *(__attribute__((address_space(1))) T *)p = v;
+}
+__device__ __forceinline__ float a_float(uint32_t u) { return __builtin_bit_cast(float, u); }
+__device__ __forceinline__ uint32_t a_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
+
+struct F32 {};
+struct Bf16 {};
+template <typename T>
+constexpr uint32_t kEntry = __is_same(T, F32) ? 4 : 2;
+
+// Entries col .. col + 7 of the row at `row`, of which `cols` exist; the others are zero.
+template <typename T>
+__device__ __forceinline__ void load8(const void *row, uint64_t col, uint64_t cols, float (&v)[8]) {
+  const uint8_t *p = static_cast<const uint8_t *>(row) + col * kEntry<T>;
+  if (col + 8 <= cols) {
+    if constexpr (__is_same(T, F32)) {
+      const af32x4 a = a_ld<af32x4_any>(p), b = a_ld<af32x4_any>(p + 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    } else {
+      const a32x4 a = a_ld<a32x4_any>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { v[2 * i] = a_float(a[i] << 16); v[2 * i + 1] = a_float(a[i] & 0xFFFF0000u); }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = 0.0f;
+      if (col + i < cols) {
+        if constexpr (__is_same(T, F32)) v[i] = a_ld<float>(p + 4 * i);
+        else v[i] = a_float((uint32_t)a_ld<uint16_t>(p + 2 * i) << 16);
+      }
+    }
+  }
+}
+// Two binary32 numbers as bf16, rounded to nearest even.
+__device__ __forceinline__ uint32_t to_bf16x2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(af32x2{a, b}, bf16x2));
+}
+template <typename T>
+__device__ __forceinline__ void store8(void *row, uint64_t col, uint64_t cols, const float (&v)[8]) {
+  uint8_t *p = static_cast<uint8_t *>(row) + col * kEntry<T>;
+  if constexpr (__is_same(T, F32)) {
+    if (col + 8 <= cols) {
+      a_st<af32x4_any>(p, af32x4{v[0], v[1], v[2], v[3]});
+      a_st<af32x4_any>(p + 16, af32x4{v[4], v[5], v[6], v[7]});
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + i < cols) a_st<float>(p + 4 * i, v[i]);
+    }
+  } else {
+    const a32x4 w = {to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
+    if (col + 8 <= cols) {
+      a_st<a32x4_any>(p, w);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + i < cols) a_st<uint16_t>(p + 2 * i, (uint16_t)(w[i / 2] >> (16 * (i % 2))));
+    }
+  }
+}
+
+// The largest of the four lanes of a block.
+__device__ __forceinline__ uint32_t block_max(uint32_t m) {
+  m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xF, 0xF, true));   // lanes 1 0 3 2
+  return max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xF, 0xF, true));  // lanes 2 3 0 1
+}
+// A lane's 8 entries of a block as codes, and the block's scale byte.  All four lanes of the block call it.  The scaled conversions
+// take the scale's exponent field; the narrowing one makes NaN of what is too large, so values are clamped first (448 is the largest).
+__device__ __forceinline__ a32x2 ckpt_encode(const float (&v)[8], uint32_t *scale) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, a_bits(v[i]) & 0x7FFFFFFFu);
+  const uint32_t top = block_max(m) >> 23;
+  const uint32_t e = max(top, kCkptLeast + 8) - 8;
+  const float X = a_float(e << 23), most = 448.0f * X;
+  a32x2 codes;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    float w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_fmed3f(v[4 * h + i], -most, most);
+    s16x2 r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, w[0], w[1], X, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, w[2], w[3], X, true);
+    codes[h] = top == 255 ? 0x7F7F7F7Fu : __builtin_bit_cast(uint32_t, r);
+  }
+  *scale = top == 255 ? 255u : e;
+  return codes;
+}
+__device__ __forceinline__ void ckpt_decode(a32x2 codes, uint32_t scale, float (&v)[8]) {
+  const float X = a_float(scale << 23);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const af32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes[h], X, false);
+    const af32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes[h], X, true);
+    v[4 * h] = lo.x; v[4 * h + 1] = lo.y; v[4 * h + 2] = hi.x; v[4 * h + 3] = hi.y;
+  }
+}
+// Chunk number `chunk` of a checkpoint (its rows back to back, each pitch / 8 chunks): codes at 8 * chunk, its block's scale behind them.
+struct CkptIn {
+  const uint8_t *codes, *scales;
+};
+struct CkptOut {
+  uint8_t *codes, *scales;
+};
+inline CkptIn ckpt_in(const void *p, uint64_t rows, uint64_t cols) {
+  if (!p) return {nullptr, nullptr};
+  return {static_cast<const uint8_t *>(p), static_cast<const uint8_t *>(p) + rows * ckpt_pitch(cols)};
+}
+inline CkptOut ckpt_out(void *p, uint64_t rows, uint64_t cols) {
+  if (!p) return {nullptr, nullptr};
+  return {static_cast<uint8_t *>(p), static_cast<uint8_t *>(p) + rows * ckpt_pitch(cols)};
+}
+__device__ __forceinline__ void ckpt_load8(const CkptIn &c, uint64_t chunk, float (&v)[8]) {
+  ckpt_decode(a_ld<a32x2>(c.codes + chunk * 8), a_ld<uint8_t>(c.scales + chunk / 4), v);
+}
+__device__ __forceinline__ void ckpt_store8(const CkptOut &c, uint64_t chunk, const float (&v)[8]) {
+  uint32_t scale;
+  const a32x2 codes = ckpt_encode(v, &scale);
+  a_st<a32x2>(c.codes + chunk * 8, codes);
+  if (chunk % 4 == 0) a_st<uint8_t>(c.scales + chunk / 4, (uint8_t)scale);
+}
+
+// Host side: what the entry points check.
+struct Region {  // rows of `bytes` bytes, `stride` bytes apart
+  const void *p;
+  uint64_t rows, bytes, stride;
+  bool written;
+};
+inline Region region(const void *p, uint64_t bytes, bool written) { return {p, 1, bytes, bytes, written}; }
+inline Region region(const dq_matrix *m, uint64_t rows, uint64_t cols, bool written) {
+  const uint64_t e = entry_bytes(m->dtype);
+  return {m->data, rows, cols * e, rows > 1 ? m->ld * e : cols * e, written};
+}
+// Whether some written region meets another one.
+bool regions_meet(const Region *r, int n);
+// A matrix that a call may read or write: DQ_OK, DQ_EINVAL or DQ_EALIGN.
+dq_status check_matrix(const dq_matrix *m, uint64_t rows, uint64_t cols);
+uint32_t device_cu_count();
+
+}  // namespace dq

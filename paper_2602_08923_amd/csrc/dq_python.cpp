@@ -5,10 +5,12 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -24,7 +26,9 @@ PyObject *g_error = nullptr;  // binding.DqError
   X(dq_mx_compress) X(dq_mx_dar_hop) X(dq_mx_decompress) X(dq_replay_run) X(dq_replay_run_steps) X(dq_sg_stats) X(dq_stats_combine) \
   X(dqx_allocate_lists) X(dq_reorder) X(dq_reorder_mean) X(dq_restore) X(dq_status_str) X(dq_last_hip_error) X(dqx_bounds_begin) \
   X(dqx_bounds_end) X(dqx_fetch) X(dqx_allocate_begin) X(dqx_allocate_end) X(dqx_stats_all) \
-  X(dqx_whole_scratch_bytes) X(dqx_whole_run)
+  X(dqx_whole_scratch_bytes) X(dqx_whole_run) X(dq_ckpt_bytes) X(dq_ckpt_save) X(dq_ckpt_load)                           \
+  X(dq_ckpt_weight_grad_scratch_bytes) X(dq_ckpt_weight_grad) X(dq_layer_norm) X(dq_layer_norm_grad_scratch_bytes)     \
+  X(dq_layer_norm_grad) X(dq_gate) X(dq_gate_grad)
 struct Lib {
 #define X(name) decltype(&::name) name = nullptr;
   DQ_SYMBOLS(X)
@@ -556,6 +560,284 @@ PyObject *py_fetch(PyObject *const *a, Py_ssize_t nargs) {  // int32 tensor of a
   for (uint32_t i = 0; i < n; ++i) PyList_SET_ITEM(list, i, PyLong_FromLong(v[i]));
   return list;
 }
+// ---- activations: tensors of any number of dimensions as matrices
+struct Act {
+  dq_matrix m = {};
+  int64_t rows = 0, cols = 0;
+};
+Act act_of(const at::Tensor &t, const char *name) {
+  if (!t.is_cuda() || t.layout() != at::kStrided) fail(std::string(name) + " must be a dense CUDA tensor");
+  if (t.dim() < 1) fail(std::string(name) + " needs a dimension");
+  Act a;
+  a.m.dtype = local_dtype(t);
+  a.m.data = t.data_ptr();
+  a.cols = t.size(-1);
+  a.rows = 1;
+  int64_t ld = a.cols;
+  for (int64_t d = t.dim() - 2; d >= 0; --d) {
+    if (t.size(d) == 0) {
+      a.rows = 0;
+      break;
+    }
+    if (t.size(d) == 1) continue;
+    if (a.rows == 1) ld = t.stride(d);
+    else if (t.stride(d) != ld * a.rows) fail(std::string(name) + ": the rows lie at one distance from each other (take a .contiguous() first)");
+    a.rows *= t.size(d);
+  }
+  if (a.rows != 0 && a.cols != 0) {
+    if (a.cols > 1 && t.stride(-1) != 1) fail(std::string(name) + ": a row's entries lie side by side (take a .contiguous() first)");
+    if (a.rows > 1 && ld < a.cols) fail(std::string(name) + ": rows must not overlap (take a .contiguous() first)");
+  }
+  a.m.ld = (uint64_t)ld;
+  return a;
+}
+// The calls below run on their tensors' device: it is the current one while they check, allocate and launch.
+struct OnDevice {
+  c10::DeviceGuard guard;
+  c10::Device device;
+  explicit OnDevice(const at::Tensor &t) : guard(cuda(t)), device(t.device()) {}
+  static c10::Device cuda(const at::Tensor &t) {
+    if (!t.is_cuda()) fail("tensors must be CUDA tensors");
+    return t.device();
+  }
+  void with(const at::Tensor &t) const {
+    if (t.device() != device) fail("the call's tensors lie on different devices");
+  }
+  void with(const at::Tensor *t) const {
+    if (t) with(*t);
+  }
+};
+void same(const Act &a, const Act &b, const char *name) {
+  if (a.rows != b.rows || a.cols != b.cols) fail(std::string(name) + " has another shape");
+  if (a.m.dtype != b.m.dtype) fail(std::string(name) + " has another type");
+}
+void *vector_of(const at::Tensor *t, int64_t n, at::ScalarType type, const char *name) {
+  if (!t) return nullptr;
+  if (t->numel() != n || t->scalar_type() != type) fail(std::string(name) + " has another length or type");
+  return ptr(*t);
+}
+at::Tensor make_shaped(at::IntArrayRef shape, at::ScalarType t, const at::Tensor &like) {
+  return unlocked([&] { return at::empty(shape, like.options().dtype(t)); });
+}
+// A checkpoint's tensor, rows and columns as three arguments.
+struct Saved {
+  const at::Tensor *data = nullptr;
+  int64_t rows = 0, cols = 0;
+};
+constexpr const char *kCkpt = "a checkpoint's data is uint8 and holds all its bytes";
+void *ckpt_ptr(const at::Tensor &t, int64_t rows, int64_t cols) {
+  if (t.scalar_type() != at::kByte || (uint64_t)t.numel() < L.dq_ckpt_bytes((uint64_t)rows, (uint64_t)cols)) fail(kCkpt);
+  return t.numel() ? ptr(t) : nullptr;
+}
+Saved saved_of(PyObject *const *a, const OnDevice &here) {
+  Saved s;
+  s.data = &tensor(a[0]);
+  here.with(s.data);
+  const long long r = PyLong_AsLongLong(a[1]), c = PyErr_Occurred() ? -1 : PyLong_AsLongLong(a[2]);
+  if (PyErr_Occurred()) throw Raised();
+  if (r < 0 || c < 0) fail("a checkpoint's rows and columns are not negative");
+  s.rows = r;
+  s.cols = c;
+  if (r && c && !L.dq_ckpt_bytes((uint64_t)r, (uint64_t)c)) fail("a checkpoint of so many rows and columns does not exist");
+  ckpt_ptr(*s.data, r, c);
+  return s;
+}
+// A new checkpoint's tensor, or the one given.
+at::Tensor ckpt_new(PyObject *given, const Act &x, const at::Tensor &like, const OnDevice &here) {
+  const uint64_t bytes = L.dq_ckpt_bytes((uint64_t)x.rows, (uint64_t)x.cols);
+  if (x.rows && x.cols && !bytes) fail("a checkpoint of so many rows and columns does not exist");
+  if (given == Py_None) return make((int64_t)bytes, at::kByte, like);
+  const at::Tensor &t = tensor(given);
+  here.with(t);
+  ckpt_ptr(t, x.rows, x.cols);
+  return t;
+}
+int64_t flag(PyObject *o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Raised();
+  return v;
+}
+PyObject *tuple(std::initializer_list<PyObject *> v) {
+  PyObject *t = PyTuple_New((Py_ssize_t)v.size());
+  Py_ssize_t i = 0;
+  for (PyObject *o : v) PyTuple_SET_ITEM(t, i++, o);
+  return t;
+}
+PyObject *none() {
+  Py_INCREF(Py_None);
+  return Py_None;
+}
+
+PyObject *py_ckpt_save(PyObject *const *a, Py_ssize_t nargs) {  // x, out -> data, rows, cols
+  DQ_ARGS(2)
+  const at::Tensor &x = tensor(a[0]);
+  const OnDevice here(x);
+  const Act m = act_of(x, "x");
+  const at::Tensor out = ckpt_new(a[1], m, x, here);
+  void *o = ckpt_ptr(out, m.rows, m.cols), *s = stream();
+  CALL(dq_ckpt_save(&m.m, m.rows, m.cols, o, s));
+  return tuple({give(a[1], out), PyLong_FromLongLong(m.rows), PyLong_FromLongLong(m.cols)});
+}
+PyObject *py_ckpt_load(PyObject *const *a, Py_ssize_t nargs) {  // data, rows, cols, bf16 (None: another type), out
+  DQ_ARGS(5)
+  const OnDevice here(tensor(a[0]));
+  const Saved c = saved_of(a, here);
+  if (a[3] == Py_None) fail("checkpoints are read as float32 or bfloat16");
+  const at::Tensor out = a[4] == Py_None ? make_shaped({c.rows, c.cols}, flag(a[3]) ? at::kBFloat16 : at::kFloat, *c.data) : tensor(a[4]);
+  here.with(out);
+  const Act m = act_of(out, "out");
+  if (m.rows != c.rows || m.cols != c.cols) fail("out has another shape");
+  void *i = ckpt_ptr(*c.data, c.rows, c.cols), *s = stream();
+  CALL(dq_ckpt_load(i, c.rows, c.cols, &m.m, s));
+  return give(a[4], out);
+}
+PyObject *py_ckpt_weight_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, data, rows, cols, out, bias, bias_out, accumulate
+  DQ_ARGS(8)
+  const at::Tensor &dy = tensor(a[0]);
+  const OnDevice here(dy);
+  const Act g = act_of(dy, "dy");
+  const Saved x = saved_of(a + 1, here);
+  if (x.rows != g.rows) fail("dy has another number of rows than the checkpoint");
+  const bool accumulate = flag(a[7]), bias = flag(a[5]) || a[6] != Py_None;
+  if (accumulate && (a[4] == Py_None || (bias && a[6] == Py_None))) fail("accumulate adds to out and bias_out: give them");
+  const at::Tensor out = a[4] == Py_None ? make_shaped({g.cols, x.cols}, dy.scalar_type(), dy) : tensor(a[4]);
+  here.with(out);
+  const Act w = act_of(out, "out");
+  if (w.rows != g.cols || w.cols != x.cols) fail("out has another shape");
+  at::Tensor db;
+  if (bias) {
+    db = a[6] == Py_None ? make(g.cols, out.scalar_type(), out) : tensor(a[6]);
+    here.with(db);
+  }
+  void *d = bias ? vector_of(&db, g.cols, out.scalar_type(), "bias_out") : nullptr;
+  at::Tensor scratch;  // free again when the call returns: what is enqueued on its stream next may have the memory
+  const size_t bytes = L.dq_ckpt_weight_grad_scratch_bytes(g.m.dtype, g.rows, g.cols, x.cols);
+  if (bytes) scratch = make((int64_t)bytes, at::kByte, dy);
+  void *t = bytes ? scratch.data_ptr() : nullptr, *i = ckpt_ptr(*x.data, x.rows, x.cols), *s = stream();
+  CALL(dq_ckpt_weight_grad(&g.m, i, g.rows, g.cols, x.cols, &w.m, d, accumulate, t, bytes, s));
+  return bias ? pair(give(a[4], out), give(a[6], db)) : give(a[4], out);
+}
+at::ScalarType weight_type(const at::Tensor *weight, const at::Tensor *bias) {
+  const at::Tensor *t = weight ? weight : bias;
+  if (!t) return at::kFloat;
+  if (t->scalar_type() != at::kFloat && t->scalar_type() != at::kBFloat16) fail("weights must be float32 or bfloat16");
+  return t->scalar_type();
+}
+dq_dtype dtype_of(at::ScalarType t) { return t == at::kFloat ? DQ_F32 : DQ_BF16; }
+PyObject *py_layer_norm(PyObject *const *a, Py_ssize_t nargs) {  // x, weight, bias, eps, save, out
+  DQ_ARGS(6)
+  const at::Tensor &x = tensor(a[0]), *weight = tensor_or_null(a[1]), *bias = tensor_or_null(a[2]);
+  const OnDevice here(x);
+  here.with(weight);
+  here.with(bias);
+  const Act m = act_of(x, "x");
+  const at::ScalarType wt = weight_type(weight, bias);
+  void *w = vector_of(weight, m.cols, wt, "weight"), *b = vector_of(bias, m.cols, wt, "bias");
+  const double eps = PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred()) throw Raised();
+  const bool save = flag(a[4]);
+  const at::Tensor out = a[5] == Py_None ? make_shaped(x.sizes(), x.scalar_type(), x) : tensor(a[5]);
+  here.with(out);
+  const Act y = act_of(out, "out");
+  same(m, y, "out");
+  at::Tensor ckpt, mean, rstd;
+  if (save) {
+    ckpt = ckpt_new(Py_None, m, x, here);
+    mean = make(m.rows, at::kFloat, x);
+    rstd = make(m.rows, at::kFloat, x);
+  }
+  void *c = save ? ckpt.data_ptr() : nullptr, *s = stream();
+  float *mu = save ? as<float>(mean.data_ptr()) : nullptr, *rs = save ? as<float>(rstd.data_ptr()) : nullptr;
+  CALL(dq_layer_norm(&m.m, m.rows, m.cols, w, b, dtype_of(wt), (float)eps, &y.m, c, mu, rs, s));
+  if (!save) return give(a[5], out);
+  return tuple({give(a[5], out), wrap(ckpt), PyLong_FromLongLong(m.rows), PyLong_FromLongLong(m.cols), wrap(mean), wrap(rstd)});
+}
+PyObject *py_layer_norm_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, data, rows, cols, mean, rstd, weight, out, weight_out, bias_out, accumulate
+  DQ_ARGS(11)
+  const at::Tensor &dy = tensor(a[0]), &mean = tensor(a[4]), &rstd = tensor(a[5]), *weight = tensor_or_null(a[6]);
+  const OnDevice here(dy);
+  here.with(mean);
+  here.with(rstd);
+  here.with(weight);
+  const Act g = act_of(dy, "dy");
+  const Saved x = saved_of(a + 1, here);
+  if (x.rows != g.rows || x.cols != g.cols) fail("dy has another shape than the checkpoint");
+  void *mu = vector_of(&mean, g.rows, at::kFloat, "mean"), *rs = vector_of(&rstd, g.rows, at::kFloat, "rstd");
+  const at::ScalarType wt = weight_type(weight, nullptr);
+  void *w = vector_of(weight, g.cols, wt, "weight");
+  const bool accumulate = flag(a[10]);
+  if (!weight && (a[8] != Py_None || a[9] != Py_None || accumulate)) fail("without a weight there are no gradients of weight and bias");
+  if (accumulate && (a[8] == Py_None || a[9] == Py_None)) fail("accumulate adds to weight_out and bias_out: give them");
+  const at::Tensor out = a[7] == Py_None ? make_shaped(dy.sizes(), dy.scalar_type(), dy) : tensor(a[7]);
+  here.with(out);
+  const Act d = act_of(out, "out");
+  same(g, d, "out");
+  at::Tensor dw, db, scratch;
+  void *pw = nullptr, *pb = nullptr, *t = nullptr;
+  size_t bytes = 0;
+  if (weight) {
+    dw = a[8] == Py_None ? make(g.cols, wt, dy) : tensor(a[8]);
+    db = a[9] == Py_None ? make(g.cols, wt, dy) : tensor(a[9]);
+    here.with(dw);
+    here.with(db);
+    pw = vector_of(&dw, g.cols, wt, "weight_out");
+    pb = vector_of(&db, g.cols, wt, "bias_out");
+    bytes = L.dq_layer_norm_grad_scratch_bytes(g.rows, g.cols);
+    if (bytes) scratch = make((int64_t)bytes, at::kByte, dy);  // free again when the call returns, as above
+    t = bytes ? scratch.data_ptr() : nullptr;
+  }
+  void *c = ckpt_ptr(*x.data, x.rows, x.cols), *s = stream();
+  CALL(dq_layer_norm_grad(&g.m, c, as<float>(mu), as<float>(rs), g.rows, g.cols, w, dtype_of(wt), &d.m, pw, pb, accumulate, t, bytes, s));
+  if (!weight) return tuple({give(a[7], out), none(), none()});
+  return tuple({give(a[7], out), give(a[8], dw), give(a[9], db)});
+}
+PyObject *py_gate(PyObject *const *a, Py_ssize_t nargs) {  // kind, z, u, save, out
+  DQ_ARGS(5)
+  const dq_activation kind = (dq_activation)number(a[0]);
+  const at::Tensor &z = tensor(a[1]), *u = tensor_or_null(a[2]);
+  const OnDevice here(z);
+  here.with(u);
+  const Act m = act_of(z, "z"), n = u ? act_of(*u, "u") : Act();
+  if (u) same(m, n, "u");
+  const bool save = flag(a[3]);
+  const at::Tensor out = a[4] == Py_None ? make_shaped(z.sizes(), z.scalar_type(), z) : tensor(a[4]);
+  here.with(out);
+  const Act h = act_of(out, "out");
+  same(m, h, "out");
+  at::Tensor cz, cu;
+  if (save) cz = ckpt_new(Py_None, m, z, here);
+  if (save && u) cu = ckpt_new(Py_None, m, z, here);
+  void *pz = save ? cz.data_ptr() : nullptr, *pu = save && u ? cu.data_ptr() : nullptr, *s = stream();
+  CALL(dq_gate(kind, &m.m, u ? &n.m : nullptr, m.rows, m.cols, &h.m, pz, pu, s));
+  if (!save) return give(a[4], out);
+  return tuple({give(a[4], out), PyLong_FromLongLong(m.rows), PyLong_FromLongLong(m.cols), wrap(cz), u ? wrap(cu) : none()});
+}
+PyObject *py_gate_grad(PyObject *const *a, Py_ssize_t nargs) {  // kind, dh, z's data, rows, cols, u's data, z_out, u_out
+  DQ_ARGS(8)
+  const dq_activation kind = (dq_activation)number(a[0]);
+  const at::Tensor &dh = tensor(a[1]), *u = tensor_or_null(a[5]);
+  const OnDevice here(dh);
+  here.with(u);
+  const Act g = act_of(dh, "dh");
+  const Saved z = saved_of(a + 2, here);
+  if (z.rows != g.rows || z.cols != g.cols) fail("dh has another shape than the checkpoint");
+  if (!u && a[7] != Py_None) fail("there was no u");
+  const at::Tensor dz = a[6] == Py_None ? make_shaped(dh.sizes(), dh.scalar_type(), dh) : tensor(a[6]);
+  here.with(dz);
+  const Act mz = act_of(dz, "z_out");
+  same(g, mz, "z_out");
+  at::Tensor du;
+  Act mu;
+  if (u) {
+    du = a[7] == Py_None ? make_shaped(dh.sizes(), dh.scalar_type(), dh) : tensor(a[7]);
+    here.with(du);
+    mu = act_of(du, "u_out");
+    same(g, mu, "u_out");
+  }
+  void *pz = ckpt_ptr(*z.data, z.rows, z.cols), *pu = u ? ckpt_ptr(*u, z.rows, z.cols) : nullptr, *s = stream();
+  CALL(dq_gate_grad(kind, &g.m, pz, pu, g.rows, g.cols, &mz.m, u ? &mu.m : nullptr, s));
+  return pair(give(a[6], dz), u ? give(a[7], du) : none());
+}
 PyObject *py_init(PyObject *const *a, Py_ssize_t nargs) {  // path of libdq.so, DqError
   DQ_ARGS(2)
   const char *path = PyUnicode_AsUTF8(a[0]);
@@ -586,7 +868,8 @@ PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
 #define M(name) {#name, (PyCFunction)(void (*)(void))guarded<py_##name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {M(init), M(compress), M(dar_hop), M(decompress), M(decompress_restore), M(mx_compress), M(mx_dar_hop),
                          M(mx_decompress), M(replay_used), M(replay_run), M(replay_run_steps), M(sg_stats), M(stats_combine), M(allocate), M(allocate_begin), M(allocate_end),
-                         M(reorder), M(reorder_mean), M(restore), M(check_index), M(stats_all), M(whole), M(fetch), {nullptr, nullptr, 0, nullptr}};
+                         M(reorder), M(reorder_mean), M(restore), M(check_index), M(stats_all), M(whole), M(fetch), M(ckpt_save), M(ckpt_load), M(ckpt_weight_grad), M(layer_norm), M(layer_norm_grad), M(gate),
+                         M(gate_grad), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dqpy", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
