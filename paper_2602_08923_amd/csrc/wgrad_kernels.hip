@@ -22,17 +22,22 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 struct WGrad {
   Rows dy;
   CkptIn x;
-  uint64_t rows, outs, cols;
+  uint64_t rows, outs, cols, pitch;
   void *dw, *db;
-  uint64_t ld, tiles, tiles_out;
-  uint32_t accumulate;
+  uint64_t ld;
+  float *part;                // [splits][tiles][a tile's sums in the accumulators' order], then [splits][outs]: null without a split
+  uint64_t tiles;
+  uint32_t tiles_out, tiles_in, splits, accumulate;
+  uint64_t split_rows;        // tokens of a split, a multiple of the step
 };
 
 constexpr uint32_t kThreads = 256;
 
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) a32x4 lds_a32x4;
-// Tokens 0 .. 15 of 32 columns: `at` is the LDS address of the first token's first column plus the lane's part (read_at).
+typedef __attribute__((address_space(3))) float lds_float;
+
+// A lane's part of the address of 16 tokens of 32 columns.
 __device__ __forceinline__ uint32_t read_at(uint32_t stride) {
   const uint32_t l = threadIdx.x & 63u;
   return ((l >> 5) * 8 + (l & 15u) / 4) * stride + ((l >> 4) & 1u) * 32 + (l & 3u) * 8;
@@ -43,6 +48,12 @@ __device__ __forceinline__ bf16x8 read16(uint32_t at, uint32_t stride) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+// Waits for this wave's LDS accesses only, then for the block's other waves: loads from memory stay on their way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
 
 template <typename O>
 __device__ __forceinline__ void put(void *out, uint64_t at, float v, uint32_t accumulate) {
@@ -55,72 +66,396 @@ __device__ __forceinline__ void put(void *out, uint64_t at, float v, uint32_t ac
     a_st<uint16_t>(p, (uint16_t)to_bf16x2(v, v));
   }
 }
+// Eight sums of row o from column i on; cols: the row's length.
+template <typename O>
+__device__ __forceinline__ void put8(const WGrad &g, uint64_t o, uint64_t i, float (&v)[8]) {
+  uint8_t *row = static_cast<uint8_t *>(g.dw) + o * g.ld * kEntry<O>;
+  if (g.accumulate) {
+    float old[8];
+    load8<O>(row, i, g.cols, old);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += old[k];
+  }
+  store8<O>(row, i, g.cols, v);
+}
 
-// A block's tile is 64 by 64, a wave's 32 by 32.
-template <typename T, typename O>
+// A block's tile: kOut x kIn sums, kTok tokens a step; four waves, two by two, of kOut / 2 by kIn / 2 each.
+template <typename T, uint32_t OUT, uint32_t IN, uint32_t TOK>
+struct Tile {
+  static constexpr uint32_t kOut = OUT, kIn = IN, kTok = TOK;
+  static constexpr uint32_t kPlanes = __is_same(T, F32) ? 3 : 1;
+  static constexpr uint32_t kOutStride = OUT * 2 + 64, kInStride = IN * 2 + 64;        // bytes of an LDS row
+  static constexpr uint32_t kX = kPlanes * TOK * kOutStride;                           // where x's rows begin
+  static constexpr uint32_t kBuffer = kX + TOK * kInStride;
+  static constexpr uint32_t kOutLanes = OUT / 8, kOutRows = kThreads / kOutLanes, kOutLoads = TOK / kOutRows;   // 8 entries of dy a lane
+  static constexpr uint32_t kInLanes = IN / 16, kInRows = kThreads / kInLanes, kInLoads = TOK / kInRows;        // 16 codes a lane
+  static constexpr uint32_t kM = OUT / 64, kN = IN / 64;                               // products of 32 x 32 of a wave
+  static_assert(kOutStride % 256 % 128 == 64 && kInStride % 256 % 128 == 64 && kOutRows * kOutLoads == TOK && kInRows * kInLoads == TOK, "");
+};
+
+// Which of dy's columns column c of a tile holds (see `shift` below); outs or more: none, or one that another column holds too.
+template <bool SMALL>
+__device__ __forceinline__ uint64_t column(uint64_t outs, uint64_t o0, uint32_t c) {
+  const uint64_t chunk = o0 + (c & ~7u);
+  if (SMALL || chunk >= outs || chunk + 8 <= outs) return o0 + c;
+  const uint32_t shift = (uint32_t)(chunk + 8 - outs);
+  return (c & 7u) < shift ? outs : o0 + c - shift;
+}
+// What a lane has on its way from memory: its part of a step.
+template <typename T, typename S>
+struct Stage {
+  a32x4 dy[S::kOutLoads * (__is_same(T, F32) ? 2 : 1)], x[S::kInLoads];
+  uint32_t scale[S::kInLoads];
+};
+
+// A block's walk over the tokens, one tile at a time.  Steps go through two buffers in LDS: while the matrix cores read one, the next
+// step's operands go to the other, from registers that hold them since the step before; what the registers get meanwhile has a
+// whole step to arrive.  SMALL: fewer than 8 outs, loaded entry by entry.
+template <typename T, typename O, typename S, bool SMALL>
+struct Walker {
+  const WGrad &g;
+  const uint32_t base, wave, out_row, out_col, in_row, in_col;
+  uint64_t o0, i0, first, end;
+  const uint8_t *dy, *codes, *scales;  // this lane's first row of a step
+  uint64_t dy_row, dy_step;            // bytes from a row to the next, from a step to the next
+  bool bias;
+  Stage<T, S> st;
+  float sums[8];
+  f32x16 acc[S::kM][S::kN];
+
+  __device__ __forceinline__ Walker(const WGrad &g_, uint32_t lds)
+      : g(g_), base(lds), wave(threadIdx.x >> 6), out_row(threadIdx.x / S::kOutLanes), out_col(threadIdx.x % S::kOutLanes * 8),
+        in_row(threadIdx.x / S::kInLanes), in_col(threadIdx.x % S::kInLanes * 16) {}
+
+  __device__ __forceinline__ void begin(uint64_t tile, uint64_t from, uint64_t to) {
+    o0 = tile / g.tiles_in * S::kOut;
+    i0 = tile % g.tiles_in * S::kIn;
+    first = from;
+    end = to;
+    bias = g.db && i0 == 0;
+    // A lane's 8 entries of dy that would pass the row's end are taken up to it: they hold earlier columns then (see column()).
+    // Columns beyond the matrices are read as their first ones and not stored.
+    const uint64_t o = o0 + out_col;
+    const uint64_t from_o = SMALL ? 0 : o >= g.outs ? 0 : o + 8 > g.outs ? g.outs - 8 : o, from_i = i0 + in_col < g.pitch ? i0 + in_col : 0;
+    dy_row = g.dy.ld * kEntry<T>;
+    dy = static_cast<const uint8_t *>(g.dy.data) + (first + out_row) * dy_row + from_o * kEntry<T>;
+    codes = g.x.codes + (first + in_row) * g.pitch + from_i;
+    scales = g.x.scales + ((first + in_row) * g.pitch + from_i) / kCkptBlock;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[i] = 0.0f;
+#pragma unroll
+    for (uint32_t m = 0; m < S::kM; ++m)
+#pragma unroll
+      for (uint32_t n = 0; n < S::kN; ++n) acc[m][n] = f32x16{};
+  }
+
+  // LAST: the step may end behind the last token; tokens there are read as the last one.
+  template <bool LAST>
+  __device__ __forceinline__ void load(uint32_t step) {
+    const uint64_t t0 = first + (uint64_t)step * S::kTok;
+#pragma unroll
+    for (uint32_t j = 0; j < S::kOutLoads; ++j) {
+      uint64_t ahead = (uint64_t)step * S::kTok + j * S::kOutRows;
+      if (LAST && t0 + out_row + j * S::kOutRows >= end) ahead = end - 1 - first - out_row;  // (modulo 2^64)
+      const uint8_t *p = dy + ahead * dy_row;
+      if constexpr (SMALL) {
+        float v[8];
+        load8<T>(p, o0 + out_col, g.outs, v);
+        if constexpr (__is_same(T, F32)) {
+          st.dy[2 * j] = a32x4{a_bits(v[0]), a_bits(v[1]), a_bits(v[2]), a_bits(v[3])};
+          st.dy[2 * j + 1] = a32x4{a_bits(v[4]), a_bits(v[5]), a_bits(v[6]), a_bits(v[7])};
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st.dy[j][i] = high_halves(a_bits(v[2 * i]), a_bits(v[2 * i + 1]));
+        }
+      } else if constexpr (__is_same(T, F32)) {
+        st.dy[2 * j] = a_ld<a32x4_any>(p);
+        st.dy[2 * j + 1] = a_ld<a32x4_any>(p + 16);
+      } else {
+        st.dy[j] = a_ld<a32x4_any>(p);
+      }
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < S::kInLoads; ++j) {
+      uint64_t ahead = (uint64_t)step * S::kTok + j * S::kInRows;
+      if (LAST && t0 + in_row + j * S::kInRows >= end) ahead = end - 1 - first - in_row;
+      st.x[j] = a_ld<a32x4>(codes + ahead * g.pitch);
+      st.scale[j] = a_ld<uint8_t>(scales + ahead * (g.pitch / kCkptBlock));
+    }
+  }
+  // The last step's tokens behind the end count nothing.
+  __device__ __forceinline__ void cut(uint32_t step) {
+    const uint64_t t0 = first + (uint64_t)step * S::kTok;
+    constexpr uint32_t n = __is_same(T, F32) ? 2 : 1;
+#pragma unroll
+    for (uint32_t j = 0; j < S::kOutLoads; ++j) {
+      const bool none = t0 + out_row + j * S::kOutRows >= end;
+#pragma unroll
+      for (uint32_t h = 0; h < n; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.dy[n * j + h][i] = none ? 0u : st.dy[n * j + h][i];
+    }
+  }
+  __device__ __forceinline__ void add_bias() {
+#pragma unroll
+    for (uint32_t j = 0; j < S::kOutLoads; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (__is_same(T, F32)) {
+          sums[i] += a_float(st.dy[2 * j][i]);
+          sums[4 + i] += a_float(st.dy[2 * j + 1][i]);
+        } else {
+          sums[2 * i] += a_float(st.dy[j][i] << 16);
+          sums[2 * i + 1] += a_float(st.dy[j][i] & 0xFFFF0000u);
+        }
+      }
+  }
+  __device__ __forceinline__ void store(uint32_t step) {
+    const uint32_t to = base + (step & 1u) * S::kBuffer;
+    const uint32_t put_dy = to + out_row * S::kOutStride + out_col * 2, put_x = to + S::kX + in_row * S::kInStride + in_col * 2;
+#pragma unroll
+    for (uint32_t j = 0; j < S::kOutLoads; ++j) {
+      if constexpr (__is_same(T, F32)) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = a_float(st.dy[2 * j][i]); v[4 + i] = a_float(st.dy[2 * j + 1][i]); }
+#pragma unroll
+        for (uint32_t p = 0; p < S::kPlanes; ++p) {
+          a32x4 w;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = high_halves(a_bits(v[2 * i]), a_bits(v[2 * i + 1]));
+          *reinterpret_cast<lds_a32x4 *>(put_dy + (p * S::kTok + j * S::kOutRows) * S::kOutStride) = w;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] -= a_float(a_bits(v[i]) & 0xFFFF0000u);
+        }
+      } else {
+        *reinterpret_cast<lds_a32x4 *>(put_dy + j * S::kOutRows * S::kOutStride) = st.dy[j];
+      }
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < S::kInLoads; ++j) {
+      const float X = a_float(st.scale[j] << 23);
+      a32x4 w[2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[i / 2][i % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(st.x[j][i], X, false));
+        w[i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(st.x[j][i], X, true));
+      }
+      const uint32_t at = put_x + j * S::kInRows * S::kInStride;
+      *reinterpret_cast<lds_a32x4 *>(at) = w[0];
+      *reinterpret_cast<lds_a32x4 *>(at + 16) = w[1];
+    }
+  }
+  __device__ __forceinline__ void multiply(uint32_t step) {
+    const uint32_t from = base + (step & 1u) * S::kBuffer, wo = (wave & 1u) * (S::kOut / 2), wi = (wave >> 1) * (S::kIn / 2);
+    const uint32_t get_dy = from + wo * 2 + read_at(S::kOutStride), get_x = from + S::kX + wi * 2 + read_at(S::kInStride);
+#pragma unroll
+    for (uint32_t k = 0; k < S::kTok; k += 16) {
+      bf16x8 b[S::kN];
+#pragma unroll
+      for (uint32_t n = 0; n < S::kN; ++n) b[n] = read16(get_x + k * S::kInStride + n * 64, S::kInStride);
+#pragma unroll
+      for (uint32_t p = 0; p < S::kPlanes; ++p) {
+        bf16x8 a[S::kM];
+#pragma unroll
+        for (uint32_t m = 0; m < S::kM; ++m) a[m] = read16(get_dy + (p * S::kTok + k) * S::kOutStride + m * 64, S::kOutStride);
+#pragma unroll
+        for (uint32_t m = 0; m < S::kM; ++m)
+#pragma unroll
+          for (uint32_t n = 0; n < S::kN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[m], b[n], acc[m][n], 0, 0, 0);
+      }
+    }
+  }
+  __device__ __forceinline__ void walk() {
+    const uint32_t steps = end > first ? (uint32_t)((end - first + S::kTok - 1) / S::kTok) : 0u;
+    if (steps == 0) return;
+    const uint32_t last = steps - 1;
+    if (last == 0) {
+      load<true>(0);
+      cut(0);
+    } else {
+      load<false>(0);
+    }
+    if (bias) add_bias();
+    store(0);
+    if (last == 1) load<true>(1);
+    else if (last > 1) load<false>(1);
+    lds_barrier();
+    uint32_t step = 0;
+    for (; step + 2 < last; ++step) {
+      if (bias) add_bias();
+      store(step + 1);
+      load<false>(step + 2);
+      multiply(step);
+      lds_barrier();
+    }
+    for (; step < last; ++step) {
+      if (step + 1 == last) cut(last);
+      if (bias) add_bias();
+      store(step + 1);
+      if (step + 2 == last) load<true>(last);
+      multiply(step);
+      lds_barrier();
+    }
+    multiply(last);
+  }
+  // A product's 32 x 32 sums go through a patch of LDS of the wave's own, so that a lane has 16 of a row.
+  __device__ __forceinline__ void put_tile() {
+    constexpr uint32_t kRow = 144;
+    uint32_t l = threadIdx.x & 63u;
+    asm volatile("" : "+v"(l));  // what follows from it is worked out here, not kept in registers through the steps
+    const uint32_t patch = base + wave * (32 * kRow), to = patch + 4 * (l >> 5) * kRow + (l & 31u) * 4, from = patch + (l >> 1) * kRow + (l & 1u) * 64;
+    const uint32_t c = (wave & 1u) * (S::kOut / 2) + (l >> 1);
+    const uint64_t i = i0 + (wave >> 1) * (S::kIn / 2) + (l & 1u) * 16;
+#pragma unroll
+    for (uint32_t m = 0; m < S::kM; ++m) {
+      const uint64_t o = column<SMALL>(g.outs, o0, c + m * 32);
+#pragma unroll
+      for (uint32_t n = 0; n < S::kN; ++n) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t r = 0; r < 16; ++r) *reinterpret_cast<lds_float *>(to + (8 * (r / 4) + r % 4) * kRow) = acc[m][n][r];
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        float v[2][8];
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) {
+          const a32x4 w = *reinterpret_cast<lds_a32x4 *>(from + q * 16);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[q / 2][q % 2 * 4 + k] = a_float(w[k]);
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (o < g.outs) {
+#pragma unroll
+          for (uint32_t h = 0; h < 2; ++h)
+            if (i + n * 32 + h * 8 < g.cols) put8<O>(g, o, i + n * 32 + h * 8, v[h]);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void put_part(uint64_t unit) {
+    float *p = g.part + (unit * 4 + wave) * (uint64_t)(S::kM * S::kN * 1024) + (threadIdx.x & 63u) * 4;
+#pragma unroll
+    for (uint32_t m = 0; m < S::kM; ++m)
+#pragma unroll
+      for (uint32_t n = 0; n < S::kN; ++n)
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q)
+          a_st<af32x4>(p + ((m * S::kN + n) * 4 + q) * 256, af32x4{acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]});
+  }
+  // The lanes of a column, through LDS.
+  __device__ __forceinline__ void put_bias(uint64_t units, uint32_t split) {
+    const uint32_t to = base + (out_row * S::kOut + out_col) * 4;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<lds_float *>(to + 4 * i) = sums[i];
+    lds_barrier();
+    for (uint32_t c = threadIdx.x; c < S::kOut; c += kThreads) {
+      float v = 0.0f;
+      for (uint32_t r = 0; r < S::kOutRows; ++r) v += *reinterpret_cast<lds_float *>(base + (r * S::kOut + c) * 4);
+      const uint64_t o = column<SMALL>(g.outs, o0, c);
+      if (o >= g.outs) continue;
+      if (g.splits > 1) a_st<float>(g.part + units * (S::kOut * S::kIn) + split * g.outs + o, v);
+      else put<O>(g.db, o, v, g.accumulate);
+    }
+  }
+};
+
+template <typename T, typename O, typename S, bool SMALL>
 __global__ __launch_bounds__(kThreads) void k_wgrad(WGrad g) {
-  constexpr uint32_t kPlanes = __is_same(T, F32) ? 3 : 1, kTok = 32, kStride = 192;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[(kPlanes + 1) * kTok * kStride];
-  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds, xbase = base + kPlanes * kTok * kStride;
-  const uint64_t pitch = ckpt_pitch(g.cols);
-  const uint32_t wave = threadIdx.x >> 6, wo = (wave & 1u) * 32, wi = (wave >> 1) * 32;
-  const uint32_t tok = threadIdx.x >> 3, chunk = (threadIdx.x & 7u) * 8;
-  bf16x8 ones;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
-  for (uint64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
-  const uint64_t o0 = tile % g.tiles_out * 64, i0 = tile / g.tiles_out * 64;
-  const bool bias = g.db && i0 == 0 && wi == 0;
-  f32x16 acc = {}, sums = {};
-  for (uint64_t t0 = 0; t0 < g.rows; t0 += kTok) {
-    const uint64_t t = t0 + tok;
-    float v[8] = {};
-    a32x4 x = {0u, 0u, 0u, 0u};
-    if (t < g.rows) {
-      load8<T>(static_cast<const uint8_t *>(g.dy.data) + t * g.dy.ld * kEntry<T>, o0 + chunk, g.outs, v);
-      if (i0 + chunk < pitch) {
-        float xv[8];
-        ckpt_load8(g.x, (t * pitch + i0 + chunk) / 8, xv);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = high_halves(a_bits(xv[2 * i]), a_bits(xv[2 * i + 1]));
-      }
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * S::kBuffer];
+  Walker<T, O, S, SMALL> w(g, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds);
+  const uint64_t units = g.tiles * g.splits;
+  for (uint64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const uint32_t split = (uint32_t)(unit / g.tiles);
+    const uint64_t first = split * g.split_rows;
+    w.begin(unit % g.tiles, first, first + g.split_rows < g.rows ? first + g.split_rows : g.rows);
+    w.walk();
+    lds_barrier();
+    if (g.splits > 1) w.put_part(unit);
+    else w.put_tile();
+    if (w.bias) {
+      lds_barrier();
+      w.put_bias(units, split);
     }
-    __syncthreads();
-#pragma unroll
-    for (uint32_t p = 0; p < kPlanes; ++p) {
-      a32x4 w;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = high_halves(a_bits(v[2 * i]), a_bits(v[2 * i + 1]));
-      *reinterpret_cast<lds_a32x4 *>(base + (p * kTok + tok) * kStride + chunk * 2) = w;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] -= a_float(a_bits(v[i]) & 0xFFFF0000u);
-    }
-    *reinterpret_cast<lds_a32x4 *>(xbase + tok * kStride + chunk * 2) = x;
-    __syncthreads();
-#pragma unroll
-    for (uint32_t k = 0; k < kTok; k += 16) {
-      const bf16x8 b = read16(xbase + k * kStride + wi * 2 + read_at(kStride), kStride);
-#pragma unroll
-      for (uint32_t p = 0; p < kPlanes; ++p) {
-        const bf16x8 a = read16(base + (p * kTok + k) * kStride + wo * 2 + read_at(kStride), kStride);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
-        if (bias) sums = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, ones, sums, 0, 0, 0);
-      }
-    }
-  }
-  const uint32_t l = threadIdx.x & 63u;
-  const uint64_t i = i0 + wi + (l & 31u);
-#pragma unroll
-  for (uint32_t r = 0; r < 16; ++r) {
-    const uint64_t o = o0 + wo + 8 * (r / 4) + 4 * (l >> 5) + r % 4;
-    if (o >= g.outs) continue;
-    if (i < g.cols) put<O>(g.dw, o * g.ld + i, acc[r], g.accumulate);
-    if (bias && (l & 31u) == 0) put<O>(g.db, o, sums[r], g.accumulate);
-  }
+    lds_barrier();  // the next tile's steps go where this one's sums went
   }
 }
 
+// The splits' sums, in their order.  A thread has four of a tile, as a lane of the kernel above had them.
+template <typename O, typename S, bool SMALL>
+__global__ __launch_bounds__(kThreads) void k_wgrad_join(WGrad g) {
+  constexpr uint64_t kQuads = S::kOut * S::kIn / 4;
+  const uint64_t quads = g.tiles * kQuads, all = quads + (g.db ? g.outs : 0);
+  for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (uint64_t)gridDim.x * kThreads) {
+    if (i < quads) {
+      af32x4 v = a_ld<af32x4>(g.part + i * 4);
+      for (uint32_t s = 1; s < g.splits; ++s) v += a_ld<af32x4>(g.part + (s * quads + i) * 4);
+      const uint64_t tile = i / kQuads;
+      const uint32_t k = (uint32_t)(i % kQuads), l = k & 63u, q = (k >> 6) & 3u, mn = (k >> 8) % (S::kM * S::kN), wave = (k >> 8) / (S::kM * S::kN);
+      const uint32_t row = (wave & 1u) * (S::kOut / 2) + mn / S::kN * 32 + 8 * q + 4 * (l >> 5), col = (wave >> 1) * (S::kIn / 2) + mn % S::kN * 32 + (l & 31u);
+#pragma unroll
+      for (uint32_t r = 0; r < 4; ++r) {
+        const uint64_t o = column<SMALL>(g.outs, tile / g.tiles_in * S::kOut, row + r), i = tile % g.tiles_in * S::kIn + col;
+        if (o < g.outs && i < g.cols) put<O>(g.dw, o * g.ld + i, v[r], g.accumulate);
+      }
+    } else {
+      const float *p = g.part + g.splits * quads * 4 + (i - quads);
+      float v = 0.0f;
+      for (uint32_t s = 0; s < g.splits; ++s) v += a_ld<float>(p + s * g.outs);
+      put<O>(g.db, i - quads, v, g.accumulate);
+    }
+  }
+}
+
+// How a product is cut: the tile, and the tokens into splits.
+struct Cut {
+  uint32_t size;     // 0: 64 x 64, 1: 128 x 128, 2: 256 x 256
+  uint32_t splits;
+  uint64_t tiles_out, tiles_in, split_rows;
+};
+constexpr uint32_t kEdges[3] = {64, 128, 256}, kToks[2][3] = {{64, 32, 32}, {64, 64, 64}};  // [bf16][size]
+
+Cut cut_of(dq_dtype dtype, uint64_t rows, uint64_t outs, uint64_t cols) {
+  const uint64_t cus = 256;
+  Cut c;
+  c.size = 2;
+  if (outs < 8) c.size = 0;
+  while (c.size > 0 && ((outs + kEdges[c.size] - 1) / kEdges[c.size] * ((cols + kEdges[c.size] - 1) / kEdges[c.size])) < 64) --c.size;
+  const uint32_t e = kEdges[c.size], tok = kToks[dtype == DQ_BF16][c.size];
+  c.tiles_out = (outs + e - 1) / e;
+  c.tiles_in = (cols + e - 1) / e;
+  const uint64_t tiles = c.tiles_out * c.tiles_in, steps = (rows + tok - 1) / tok;
+  uint64_t splits = tiles >= cus ? 1 : cus / tiles;
+  if (splits > steps / 4) splits = steps / 4;
+  if (splits < 1) splits = 1;
+  const uint64_t each = (steps + splits - 1) / splits;
+  c.splits = each ? (uint32_t)((steps + each - 1) / each) : 1u;
+  if (c.splits < 1) c.splits = 1;
+  c.split_rows = each * tok;
+  return c;
+}
+
 bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+template <typename T, typename O, typename S, bool SMALL>
+hipError_t run(const WGrad &g, hipStream_t s) {
+  const uint64_t units = g.tiles * g.splits;
+  hipLaunchKernelGGL((k_wgrad<T, O, S, SMALL>), dim3((uint32_t)(units < 65536 ? units : 65536)), dim3(kThreads), 0, s, g);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || g.splits == 1) return e;
+  const uint64_t blocks = (g.tiles * (S::kOut * S::kIn / 4) + (g.db ? g.outs : 0) + kThreads - 1) / kThreads;
+  hipLaunchKernelGGL((k_wgrad_join<O, S, SMALL>), dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(kThreads), 0, s, g);
+  return hipGetLastError();
+}
+template <typename T, typename O>
+hipError_t run_cut(const Cut &c, const WGrad &g, hipStream_t s) {
+  constexpr int b = __is_same(T, Bf16);
+  if (g.outs < 8) return run<T, O, Tile<T, 64, 64, kToks[b][0]>, true>(g, s);
+  if (c.size == 0) return run<T, O, Tile<T, 64, 64, kToks[b][0]>, false>(g, s);
+  if (c.size == 1) return run<T, O, Tile<T, 128, 128, kToks[b][1]>, false>(g, s);
+  return run<T, O, Tile<T, 256, 256, kToks[b][2]>, false>(g, s);
+}
 
 }  // namespace
 }  // namespace dq
@@ -136,8 +471,10 @@ using namespace dq;
 extern "C" {
 
 size_t dq_ckpt_weight_grad_scratch_bytes(dq_dtype dtype, uint64_t rows, uint64_t outs, uint64_t cols) {
-  (void)dtype; (void)rows; (void)outs; (void)cols;
-  return 0;
+  if (rows == 0 || outs == 0 || cols == 0 || (rows | outs | cols) >> 31) return 0;
+  const Cut c = cut_of(dtype, rows, outs, cols);
+  if (c.splits == 1) return 0;
+  return (size_t)(c.splits * (c.tiles_out * c.tiles_in * kEdges[c.size] * kEdges[c.size] + outs) * 4);
 }
 
 dq_status dq_ckpt_weight_grad(const dq_matrix *dy, const void *ckpt, uint64_t rows, uint64_t outs, uint64_t cols, const dq_matrix *dw, void *db,
@@ -158,14 +495,27 @@ dq_status dq_ckpt_weight_grad(const dq_matrix *dy, const void *ckpt, uint64_t ro
                       region(db, outs * ob, true), region(need ? scratch : nullptr, need, true)};
   if (regions_meet(r, 5)) return DQ_EINVAL;
   if (rows == 0 && accumulate) return DQ_OK;
-  const WGrad g = {{dy->data, dy->ld}, ckpt_in(ckpt, rows, cols), rows, outs, cols, dw->data, db, dw->ld, (outs + 63) / 64 * ((cols + 63) / 64), (outs + 63) / 64, (uint32_t)(accumulate != 0)};
-  const uint32_t blocks = (uint32_t)(g.tiles < 65536 ? g.tiles : 65536);
-#define DQ_WGRAD(T, O) hipLaunchKernelGGL((k_wgrad<T, O>), dim3(blocks), dim3(kThreads), 0, (hipStream_t)hip_stream, g)
-  if (dy->dtype == DQ_F32 && dw->dtype == DQ_F32) DQ_WGRAD(F32, F32);
-  else if (dy->dtype == DQ_F32) DQ_WGRAD(F32, Bf16);
-  else if (dw->dtype == DQ_F32) DQ_WGRAD(Bf16, F32);
-  else DQ_WGRAD(Bf16, Bf16);
-  return hip_status(hipGetLastError());
+  const Cut c = cut_of(dy->dtype, rows, outs, cols);
+  WGrad g = {};
+  g.dy = {dy->data, dy->ld};
+  g.x = ckpt_in(ckpt, rows, cols);
+  g.rows = rows;
+  g.outs = outs;
+  g.cols = cols;
+  g.pitch = ckpt_pitch(cols);
+  g.dw = dw->data;
+  g.db = db;
+  g.ld = dw->ld;
+  g.part = static_cast<float *>(scratch);
+  g.tiles = c.tiles_out * c.tiles_in;
+  g.tiles_out = (uint32_t)c.tiles_out;
+  g.tiles_in = (uint32_t)c.tiles_in;
+  g.splits = c.splits;
+  g.split_rows = c.split_rows;
+  g.accumulate = accumulate != 0;
+  hipStream_t s = (hipStream_t)hip_stream;
+  if (dy->dtype == DQ_F32) return hip_status(dw->dtype == DQ_F32 ? run_cut<F32, F32>(c, g, s) : run_cut<F32, Bf16>(c, g, s));
+  return hip_status(dw->dtype == DQ_F32 ? run_cut<Bf16, F32>(c, g, s) : run_cut<Bf16, Bf16>(c, g, s));
 }
 
 }  // extern "C"
