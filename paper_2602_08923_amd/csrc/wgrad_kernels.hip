@@ -31,7 +31,7 @@ struct WGrad {
   uint64_t split_rows;        // tokens of a split, a multiple of the step
 };
 
-constexpr uint32_t kThreads = 256;
+constexpr uint32_t kJoinThreads = 256;
 
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) a32x4 lds_a32x4;
@@ -79,20 +79,33 @@ __device__ __forceinline__ void put8(const WGrad &g, uint64_t o, uint64_t i, flo
   store8<O>(row, i, g.cols, v);
 }
 
-// A block's tile: kOut x kIn sums, kTok tokens a step; four waves, two by two, of kOut / 2 by kIn / 2 each.
-template <typename T, uint32_t OUT, uint32_t IN, uint32_t TOK>
+// A block's tile: kOut x kIn sums, kTok tokens a step; its waves, 2 by WAVES_IN, have kWaveOut x kWaveIn each.
+template <typename T, uint32_t OUT, uint32_t IN, uint32_t TOK, uint32_t WAVES_IN>
 struct Tile {
   static constexpr uint32_t kOut = OUT, kIn = IN, kTok = TOK;
+  static constexpr uint32_t kThreads = 128 * WAVES_IN, kWaveOut = OUT / 2, kWaveIn = IN / WAVES_IN;
   static constexpr uint32_t kPlanes = __is_same(T, F32) ? 3 : 1;
   static constexpr uint32_t kOutStride = OUT * 2 + 64, kInStride = IN * 2 + 64;        // bytes of an LDS row
   static constexpr uint32_t kX = kPlanes * TOK * kOutStride;                           // where x's rows begin
   static constexpr uint32_t kBuffer = kX + TOK * kInStride;
   static constexpr uint32_t kOutLanes = OUT / 8, kOutRows = kThreads / kOutLanes, kOutLoads = TOK / kOutRows;   // 8 entries of dy a lane
   static constexpr uint32_t kInLanes = IN / 16, kInRows = kThreads / kInLanes, kInLoads = TOK / kInRows;        // 16 codes a lane
-  static constexpr uint32_t kM = OUT / 64, kN = IN / 64;                               // products of 32 x 32 of a wave
-  static_assert(kOutStride % 256 % 128 == 64 && kInStride % 256 % 128 == 64 && kOutRows * kOutLoads == TOK && kInRows * kInLoads == TOK, "");
+  static constexpr uint32_t kPieces = kOutLoads + kInLoads, kSlices = TOK / 16 * kPlanes;
+  static constexpr uint32_t kM = kWaveOut / 32, kN = kWaveIn / 32;                               // products of 32 x 32 of a wave
+  static_assert(kOutStride % 256 % 128 == 64 && kInStride % 256 % 128 == 64 && kOutRows * kOutLoads == TOK && kInRows * kInLoads == TOK && kSlices % 2 == 0 && TOK / 16 % 2 == 0, "");
 };
 
+// Tiles are numbered in strips of up to 8 along x, row by row of a strip: neighbours in number share columns of dy or of x.
+__device__ __forceinline__ uint64_t tile_strip(const WGrad &g, uint64_t tile) { return tile / (8 * (uint64_t)g.tiles_out) * 8; }
+__device__ __forceinline__ uint64_t strip_width(const WGrad &g, uint64_t strip) { return g.tiles_in - strip < 8 ? g.tiles_in - strip : 8; }
+__device__ __forceinline__ uint64_t tile_out(const WGrad &g, uint64_t tile) {
+  const uint64_t s = tile_strip(g, tile);
+  return (tile - s * g.tiles_out) / strip_width(g, s);
+}
+__device__ __forceinline__ uint64_t tile_in(const WGrad &g, uint64_t tile) {
+  const uint64_t s = tile_strip(g, tile);
+  return s + (tile - s * g.tiles_out) % strip_width(g, s);
+}
 // Which of dy's columns column c of a tile holds (see `shift` below); outs or more: none, or one that another column holds too.
 template <bool SMALL>
 __device__ __forceinline__ uint64_t column(uint64_t outs, uint64_t o0, uint32_t c) {
@@ -109,27 +122,35 @@ struct Stage {
 };
 
 // A block's walk over the tokens, one tile at a time.  Steps go through two buffers in LDS: while the matrix cores read one, the next
-// step's operands go to the other, from registers that hold them since the step before; what the registers get meanwhile has a
-// whole step to arrive.  SMALL: fewer than 8 outs, loaded entry by entry.
+// step's operands go to the other, from registers.  SMALL: fewer than 8 outs, loaded entry by entry.
 template <typename T, typename O, typename S, bool SMALL>
 struct Walker {
   const WGrad &g;
   const uint32_t base, wave, out_row, out_col, in_row, in_col;
   uint64_t o0, i0, first, end;
-  const uint8_t *dy, *codes, *scales;  // this lane's first row of a step
-  uint64_t dy_row, dy_step;            // bytes from a row to the next, from a step to the next
+  const uint8_t *dy, *codes, *scales;  // this lane's first row of the step that is loaded next
+  uint64_t dy_row;                     // bytes from a row to the next
+  uint32_t put_dy, put_x, get_dy, get_x;  // LDS addresses in the first buffer
   bool bias;
   Stage<T, S> st;
   float sums[8];
+  bf16x8 a[2][S::kM], b[2][S::kN];
   f32x16 acc[S::kM][S::kN];
 
   __device__ __forceinline__ Walker(const WGrad &g_, uint32_t lds)
       : g(g_), base(lds), wave(threadIdx.x >> 6), out_row(threadIdx.x / S::kOutLanes), out_col(threadIdx.x % S::kOutLanes * 8),
-        in_row(threadIdx.x / S::kInLanes), in_col(threadIdx.x % S::kInLanes * 16) {}
+        in_row(threadIdx.x / S::kInLanes), in_col(threadIdx.x % S::kInLanes * 16) {
+    put_dy = base + out_row * S::kOutStride + out_col * 2;
+    put_x = base + S::kX + in_row * S::kInStride + in_col * 2;
+    get_dy = base + (wave & 1u) * (S::kWaveOut * 2) + read_at(S::kOutStride);
+    get_x = base + S::kX + (wave >> 1) * (S::kWaveIn * 2) + read_at(S::kInStride);
+    // kept as they are: what is added to them below fits the instructions' offsets
+    asm volatile("" : "+v"(put_dy), "+v"(put_x), "+v"(get_dy), "+v"(get_x));
+  }
 
   __device__ __forceinline__ void begin(uint64_t tile, uint64_t from, uint64_t to) {
-    o0 = tile / g.tiles_in * S::kOut;
-    i0 = tile % g.tiles_in * S::kIn;
+    o0 = tile_out(g, tile) * S::kOut;
+    i0 = tile_in(g, tile) * S::kIn;
     first = from;
     end = to;
     bias = g.db && i0 == 0;
@@ -149,14 +170,15 @@ struct Walker {
       for (uint32_t n = 0; n < S::kN; ++n) acc[m][n] = f32x16{};
   }
 
+  // A lane's share of a step is kPieces loads: first of dy, then of the checkpoint.
   // LAST: the step may end behind the last token; tokens there are read as the last one.
   template <bool LAST>
-  __device__ __forceinline__ void load(uint32_t step) {
-    const uint64_t t0 = first + (uint64_t)step * S::kTok;
-#pragma unroll
-    for (uint32_t j = 0; j < S::kOutLoads; ++j) {
-      uint64_t ahead = (uint64_t)step * S::kTok + j * S::kOutRows;
-      if (LAST && t0 + out_row + j * S::kOutRows >= end) ahead = end - 1 - first - out_row;  // (modulo 2^64)
+  __device__ __forceinline__ void load(uint32_t step, uint32_t piece) {
+    if (piece < S::kOutLoads) {
+      const uint32_t j = piece;
+      uint64_t ahead = j * S::kOutRows;
+      const uint64_t t = first + (uint64_t)step * S::kTok + out_row;
+      if (LAST && t + ahead >= end) ahead = end - 1 - t;  // (modulo 2^64)
       const uint8_t *p = dy + ahead * dy_row;
       if constexpr (SMALL) {
         float v[8];
@@ -174,66 +196,63 @@ struct Walker {
       } else {
         st.dy[j] = a_ld<a32x4_any>(p);
       }
-    }
-#pragma unroll
-    for (uint32_t j = 0; j < S::kInLoads; ++j) {
-      uint64_t ahead = (uint64_t)step * S::kTok + j * S::kInRows;
-      if (LAST && t0 + in_row + j * S::kInRows >= end) ahead = end - 1 - first - in_row;
+    } else {
+      const uint32_t j = piece - S::kOutLoads;
+      uint64_t ahead = j * S::kInRows;
+      const uint64_t t = first + (uint64_t)step * S::kTok + in_row;
+      if (LAST && t + ahead >= end) ahead = end - 1 - t;
       st.x[j] = a_ld<a32x4>(codes + ahead * g.pitch);
       st.scale[j] = a_ld<uint8_t>(scales + ahead * (g.pitch / kCkptBlock));
     }
   }
-  // The last step's tokens behind the end count nothing.
-  __device__ __forceinline__ void cut(uint32_t step) {
-    const uint64_t t0 = first + (uint64_t)step * S::kTok;
-    constexpr uint32_t n = __is_same(T, F32) ? 2 : 1;
-#pragma unroll
-    for (uint32_t j = 0; j < S::kOutLoads; ++j) {
-      const bool none = t0 + out_row + j * S::kOutRows >= end;
-#pragma unroll
-      for (uint32_t h = 0; h < n; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) st.dy[n * j + h][i] = none ? 0u : st.dy[n * j + h][i];
-    }
+  __device__ __forceinline__ void loaded() {
+    dy += S::kTok * dy_row;
+    codes += S::kTok * g.pitch;
+    scales += S::kTok * (g.pitch / kCkptBlock);
   }
-  __device__ __forceinline__ void add_bias() {
+  // To LDS.  LAST: the last step's tokens behind the end count nothing.
+  template <bool BIAS, bool LAST>
+  __device__ __forceinline__ void store(uint32_t step, uint32_t piece) {
+    const uint32_t buffer = (step & 1u) * S::kBuffer;
+    if (piece < S::kOutLoads) {
+      const uint32_t j = piece, at = put_dy + buffer + j * S::kOutRows * S::kOutStride;
+      constexpr uint32_t n = __is_same(T, F32) ? 2 : 1;
+      if (LAST) {
+        const bool none = first + (uint64_t)step * S::kTok + j * S::kOutRows + out_row >= end;
 #pragma unroll
-    for (uint32_t j = 0; j < S::kOutLoads; ++j)
+        for (uint32_t h = 0; h < n; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (__is_same(T, F32)) {
-          sums[i] += a_float(st.dy[2 * j][i]);
-          sums[4 + i] += a_float(st.dy[2 * j + 1][i]);
-        } else {
-          sums[2 * i] += a_float(st.dy[j][i] << 16);
-          sums[2 * i + 1] += a_float(st.dy[j][i] & 0xFFFF0000u);
-        }
+          for (int i = 0; i < 4; ++i) st.dy[n * j + h][i] = none ? 0u : st.dy[n * j + h][i];
       }
-  }
-  __device__ __forceinline__ void store(uint32_t step) {
-    const uint32_t to = base + (step & 1u) * S::kBuffer;
-    const uint32_t put_dy = to + out_row * S::kOutStride + out_col * 2, put_x = to + S::kX + in_row * S::kInStride + in_col * 2;
-#pragma unroll
-    for (uint32_t j = 0; j < S::kOutLoads; ++j) {
       if constexpr (__is_same(T, F32)) {
         float v[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) { v[i] = a_float(st.dy[2 * j][i]); v[4 + i] = a_float(st.dy[2 * j + 1][i]); }
+        if constexpr (BIAS) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sums[i] += v[i];
+        }
 #pragma unroll
         for (uint32_t p = 0; p < S::kPlanes; ++p) {
           a32x4 w;
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[i] = high_halves(a_bits(v[2 * i]), a_bits(v[2 * i + 1]));
-          *reinterpret_cast<lds_a32x4 *>(put_dy + (p * S::kTok + j * S::kOutRows) * S::kOutStride) = w;
+          *reinterpret_cast<lds_a32x4 *>(at + p * S::kTok * S::kOutStride) = w;
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[i] -= a_float(a_bits(v[i]) & 0xFFFF0000u);
         }
       } else {
-        *reinterpret_cast<lds_a32x4 *>(put_dy + j * S::kOutRows * S::kOutStride) = st.dy[j];
-      }
-    }
+        *reinterpret_cast<lds_a32x4 *>(at) = st.dy[j];
+        if constexpr (BIAS) {
 #pragma unroll
-    for (uint32_t j = 0; j < S::kInLoads; ++j) {
+          for (int i = 0; i < 4; ++i) {
+            sums[2 * i] += a_float(st.dy[j][i] << 16);
+            sums[2 * i + 1] += a_float(st.dy[j][i] & 0xFFFF0000u);
+          }
+        }
+      }
+    } else {
+      const uint32_t j = piece - S::kOutLoads, at = put_x + buffer + j * S::kInRows * S::kInStride;
       const float X = a_float(st.scale[j] << 23);
       a32x4 w[2];
 #pragma unroll
@@ -241,63 +260,90 @@ struct Walker {
         w[i / 2][i % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(st.x[j][i], X, false));
         w[i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(st.x[j][i], X, true));
       }
-      const uint32_t at = put_x + j * S::kInRows * S::kInStride;
       *reinterpret_cast<lds_a32x4 *>(at) = w[0];
       *reinterpret_cast<lds_a32x4 *>(at + 16) = w[1];
     }
   }
-  __device__ __forceinline__ void multiply(uint32_t step) {
-    const uint32_t from = base + (step & 1u) * S::kBuffer, wo = (wave & 1u) * (S::kOut / 2), wi = (wave >> 1) * (S::kIn / 2);
-    const uint32_t get_dy = from + wo * 2 + read_at(S::kOutStride), get_x = from + S::kX + wi * 2 + read_at(S::kInStride);
+  // A step is kSlices rounds of kM x kN products: 16 tokens, and of a binary32 dy one of its three parts.
+  __device__ __forceinline__ void read(uint32_t step, uint32_t slice) {
+    const uint32_t buffer = (step & 1u) * S::kBuffer, k = slice / S::kPlanes * 16, p = slice % S::kPlanes;
+    if (p == 0) {
 #pragma unroll
-    for (uint32_t k = 0; k < S::kTok; k += 16) {
-      bf16x8 b[S::kN];
+      for (uint32_t n = 0; n < S::kN; ++n) b[slice / S::kPlanes % 2][n] = read16(get_x + buffer + k * S::kInStride + n * 64, S::kInStride);
+    }
 #pragma unroll
-      for (uint32_t n = 0; n < S::kN; ++n) b[n] = read16(get_x + k * S::kInStride + n * 64, S::kInStride);
+    for (uint32_t m = 0; m < S::kM; ++m) a[slice % 2][m] = read16(get_dy + buffer + (p * S::kTok + k) * S::kOutStride + m * 64, S::kOutStride);
+  }
+  __device__ __forceinline__ void multiply(uint32_t slice) {
 #pragma unroll
-      for (uint32_t p = 0; p < S::kPlanes; ++p) {
-        bf16x8 a[S::kM];
+    for (uint32_t m = 0; m < S::kM; ++m)
 #pragma unroll
-        for (uint32_t m = 0; m < S::kM; ++m) a[m] = read16(get_dy + (p * S::kTok + k) * S::kOutStride + m * 64, S::kOutStride);
+      for (uint32_t n = 0; n < S::kN; ++n)
+        acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[slice % 2][m], b[slice / S::kPlanes % 2][n], acc[m][n], 0, 0, 0);
+  }
+  // One step.  Its first slice's operands are in registers already; each slice reads the next one's while the matrix cores work, and
+  // moves its share of the next step's pieces to LDS, each followed by its load for the step after that, which has a whole step to
+  // arrive.  The barrier stands in front of the last slice: by then this step has been read and the next one written, and the next
+  // step's first operands are read behind it, in the last slice's time.
+  // STEADY: neither of the two steps that follow is the last.
+  template <bool BIAS, bool STEADY>
+  __device__ __forceinline__ void advance(uint32_t step, uint32_t last) {
 #pragma unroll
-        for (uint32_t m = 0; m < S::kM; ++m)
-#pragma unroll
-          for (uint32_t n = 0; n < S::kN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[m], b[n], acc[m][n], 0, 0, 0);
+    for (uint32_t s = 0; s < S::kSlices; ++s) {
+      if (s + 1 < S::kSlices) {
+        read(step, s + 1);
+      } else {
+        lds_barrier();
+        if (STEADY || step < last) read(step + 1, 0);
       }
+      multiply(s);
+      const uint32_t from = s * S::kPieces / (S::kSlices - 1), to = s + 1 < S::kSlices ? (s + 1) * S::kPieces / (S::kSlices - 1) : from;
+#pragma unroll
+      for (uint32_t i = from; i < to; ++i) {
+        if constexpr (STEADY) {
+          store<BIAS, false>(step + 1, i);
+          load<false>(step + 2, i);
+        } else {
+          if (step + 1 <= last) store<BIAS, true>(step + 1, i);
+          if (step + 2 <= last) load<true>(step + 2, i);
+        }
+      }
+      if (s + 2 == S::kSlices) loaded();
+      if constexpr (STEADY) mix();
     }
   }
+  // A slice's instructions in turn: the matrix cores are given the next product before the rest.
+  __device__ __forceinline__ void mix() {
+#pragma unroll
+    for (uint32_t i = 0; i < S::kM * S::kN; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS reads
+      __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);  // vector arithmetic
+      __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);  // LDS writes
+      __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // loads
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  template <bool BIAS>
   __device__ __forceinline__ void walk() {
     const uint32_t steps = end > first ? (uint32_t)((end - first + S::kTok - 1) / S::kTok) : 0u;
     if (steps == 0) return;
     const uint32_t last = steps - 1;
-    if (last == 0) {
-      load<true>(0);
-      cut(0);
-    } else {
-      load<false>(0);
+#pragma unroll
+    for (uint32_t i = 0; i < S::kPieces; ++i) load<true>(0, i);
+    loaded();
+#pragma unroll
+    for (uint32_t i = 0; i < S::kPieces; ++i) store<BIAS, true>(0, i);
+    if (last > 0) {
+#pragma unroll
+      for (uint32_t i = 0; i < S::kPieces; ++i) load<true>(1, i);
     }
-    if (bias) add_bias();
-    store(0);
-    if (last == 1) load<true>(1);
-    else if (last > 1) load<false>(1);
+    loaded();
     lds_barrier();
+    read(0, 0);
     uint32_t step = 0;
-    for (; step + 2 < last; ++step) {
-      if (bias) add_bias();
-      store(step + 1);
-      load<false>(step + 2);
-      multiply(step);
-      lds_barrier();
-    }
-    for (; step < last; ++step) {
-      if (step + 1 == last) cut(last);
-      if (bias) add_bias();
-      store(step + 1);
-      if (step + 2 == last) load<true>(last);
-      multiply(step);
-      lds_barrier();
-    }
-    multiply(last);
+    for (; step + 2 < last; ++step) advance<BIAS, true>(step, last);
+    for (; step <= last; ++step) advance<BIAS, false>(step, last);
   }
   // A product's 32 x 32 sums go through a patch of LDS of the wave's own, so that a lane has 16 of a row.
   __device__ __forceinline__ void put_tile() {
@@ -305,8 +351,8 @@ struct Walker {
     uint32_t l = threadIdx.x & 63u;
     asm volatile("" : "+v"(l));  // what follows from it is worked out here, not kept in registers through the steps
     const uint32_t patch = base + wave * (32 * kRow), to = patch + 4 * (l >> 5) * kRow + (l & 31u) * 4, from = patch + (l >> 1) * kRow + (l & 1u) * 64;
-    const uint32_t c = (wave & 1u) * (S::kOut / 2) + (l >> 1);
-    const uint64_t i = i0 + (wave >> 1) * (S::kIn / 2) + (l & 1u) * 16;
+    const uint32_t c = (wave & 1u) * S::kWaveOut + (l >> 1);
+    const uint64_t i = i0 + (wave >> 1) * S::kWaveIn + (l & 1u) * 16;
 #pragma unroll
     for (uint32_t m = 0; m < S::kM; ++m) {
       const uint64_t o = column<SMALL>(g.outs, o0, c + m * 32);
@@ -335,7 +381,7 @@ struct Walker {
     }
   }
   __device__ __forceinline__ void put_part(uint64_t unit) {
-    float *p = g.part + (unit * 4 + wave) * (uint64_t)(S::kM * S::kN * 1024) + (threadIdx.x & 63u) * 4;
+    float *p = g.part + (unit * (S::kThreads / 64) + wave) * (uint64_t)(S::kM * S::kN * 1024) + (threadIdx.x & 63u) * 4;
 #pragma unroll
     for (uint32_t m = 0; m < S::kM; ++m)
 #pragma unroll
@@ -350,7 +396,7 @@ struct Walker {
 #pragma unroll
     for (int i = 0; i < 8; ++i) *reinterpret_cast<lds_float *>(to + 4 * i) = sums[i];
     lds_barrier();
-    for (uint32_t c = threadIdx.x; c < S::kOut; c += kThreads) {
+    for (uint32_t c = threadIdx.x; c < S::kOut; c += S::kThreads) {
       float v = 0.0f;
       for (uint32_t r = 0; r < S::kOutRows; ++r) v += *reinterpret_cast<lds_float *>(base + (r * S::kOut + c) * 4);
       const uint64_t o = column<SMALL>(g.outs, o0, c);
@@ -362,15 +408,18 @@ struct Walker {
 };
 
 template <typename T, typename O, typename S, bool SMALL>
-__global__ __launch_bounds__(kThreads) void k_wgrad(WGrad g) {
+__global__ __launch_bounds__(S::kThreads) void k_wgrad(WGrad g) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * S::kBuffer];
   Walker<T, O, S, SMALL> w(g, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds);
   const uint64_t units = g.tiles * g.splits;
-  for (uint64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+  for (uint64_t turn = blockIdx.x; turn < units; turn += gridDim.x) {
+    // blocks go to the 8 XCDs in turn: each gets units that follow each other, whose operands its L2 then holds
+    const uint64_t xcd = turn % 8, each = units / 8, over = units % 8, unit = xcd * each + (xcd < over ? xcd : over) + turn / 8;
     const uint32_t split = (uint32_t)(unit / g.tiles);
     const uint64_t first = split * g.split_rows;
     w.begin(unit % g.tiles, first, first + g.split_rows < g.rows ? first + g.split_rows : g.rows);
-    w.walk();
+    if (w.bias) w.template walk<true>();
+    else w.template walk<false>();
     lds_barrier();
     if (g.splits > 1) w.put_part(unit);
     else w.put_tile();
@@ -384,19 +433,19 @@ __global__ __launch_bounds__(kThreads) void k_wgrad(WGrad g) {
 
 // The splits' sums, in their order.  A thread has four of a tile, as a lane of the kernel above had them.
 template <typename O, typename S, bool SMALL>
-__global__ __launch_bounds__(kThreads) void k_wgrad_join(WGrad g) {
+__global__ __launch_bounds__(kJoinThreads) void k_wgrad_join(WGrad g) {
   constexpr uint64_t kQuads = S::kOut * S::kIn / 4;
   const uint64_t quads = g.tiles * kQuads, all = quads + (g.db ? g.outs : 0);
-  for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (uint64_t)gridDim.x * kThreads) {
+  for (uint64_t i = (uint64_t)blockIdx.x * kJoinThreads + threadIdx.x; i < all; i += (uint64_t)gridDim.x * kJoinThreads) {
     if (i < quads) {
       af32x4 v = a_ld<af32x4>(g.part + i * 4);
       for (uint32_t s = 1; s < g.splits; ++s) v += a_ld<af32x4>(g.part + (s * quads + i) * 4);
       const uint64_t tile = i / kQuads;
       const uint32_t k = (uint32_t)(i % kQuads), l = k & 63u, q = (k >> 6) & 3u, mn = (k >> 8) % (S::kM * S::kN), wave = (k >> 8) / (S::kM * S::kN);
-      const uint32_t row = (wave & 1u) * (S::kOut / 2) + mn / S::kN * 32 + 8 * q + 4 * (l >> 5), col = (wave >> 1) * (S::kIn / 2) + mn % S::kN * 32 + (l & 31u);
+      const uint32_t row = (wave & 1u) * S::kWaveOut + mn / S::kN * 32 + 8 * q + 4 * (l >> 5), col = (wave >> 1) * S::kWaveIn + mn % S::kN * 32 + (l & 31u);
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) {
-        const uint64_t o = column<SMALL>(g.outs, tile / g.tiles_in * S::kOut, row + r), i = tile % g.tiles_in * S::kIn + col;
+        const uint64_t o = column<SMALL>(g.outs, tile_out(g, tile) * S::kOut, row + r), i = tile_in(g, tile) * S::kIn + col;
         if (o < g.outs && i < g.cols) put<O>(g.dw, o * g.ld + i, v[r], g.accumulate);
       }
     } else {
@@ -441,20 +490,20 @@ bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 template <typename T, typename O, typename S, bool SMALL>
 hipError_t run(const WGrad &g, hipStream_t s) {
   const uint64_t units = g.tiles * g.splits;
-  hipLaunchKernelGGL((k_wgrad<T, O, S, SMALL>), dim3((uint32_t)(units < 65536 ? units : 65536)), dim3(kThreads), 0, s, g);
+  hipLaunchKernelGGL((k_wgrad<T, O, S, SMALL>), dim3((uint32_t)(units < 65536 ? units : 65536)), dim3(S::kThreads), 0, s, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.splits == 1) return e;
-  const uint64_t blocks = (g.tiles * (S::kOut * S::kIn / 4) + (g.db ? g.outs : 0) + kThreads - 1) / kThreads;
-  hipLaunchKernelGGL((k_wgrad_join<O, S, SMALL>), dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(kThreads), 0, s, g);
+  const uint64_t blocks = (g.tiles * (S::kOut * S::kIn / 4) + (g.db ? g.outs : 0) + kJoinThreads - 1) / kJoinThreads;
+  hipLaunchKernelGGL((k_wgrad_join<O, S, SMALL>), dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(kJoinThreads), 0, s, g);
   return hipGetLastError();
 }
 template <typename T, typename O>
 hipError_t run_cut(const Cut &c, const WGrad &g, hipStream_t s) {
   constexpr int b = __is_same(T, Bf16);
-  if (g.outs < 8) return run<T, O, Tile<T, 64, 64, kToks[b][0]>, true>(g, s);
-  if (c.size == 0) return run<T, O, Tile<T, 64, 64, kToks[b][0]>, false>(g, s);
-  if (c.size == 1) return run<T, O, Tile<T, 128, 128, kToks[b][1]>, false>(g, s);
-  return run<T, O, Tile<T, 256, 256, kToks[b][2]>, false>(g, s);
+  if (g.outs < 8) return run<T, O, Tile<T, 64, 64, kToks[b][0], 2>, true>(g, s);
+  if (c.size == 0) return run<T, O, Tile<T, 64, 64, kToks[b][0], 2>, false>(g, s);
+  if (c.size == 1) return run<T, O, Tile<T, 128, 128, kToks[b][1], 2>, false>(g, s);
+  return run<T, O, Tile<T, 256, 256, kToks[b][2], 4>, false>(g, s);
 }
 
 }  // namespace
