@@ -89,7 +89,8 @@ struct Tile {
   static constexpr uint32_t kX = kPlanes * TOK * kOutStride;                           // where x's rows begin
   static constexpr uint32_t kBuffer = kX + TOK * kInStride;
   static constexpr uint32_t kOutLanes = OUT / 8, kOutRows = kThreads / kOutLanes, kOutLoads = TOK / kOutRows;   // 8 entries of dy a lane
-  static constexpr uint32_t kInLanes = IN / 16, kInRows = kThreads / kInLanes, kInLoads = TOK / kInRows;        // 16 codes a lane
+  static constexpr uint32_t kCodes = TOK * IN >= 16 * kThreads ? 16 : 8;                                        // a lane's, of a row
+  static constexpr uint32_t kInLanes = IN / kCodes, kInRows = kThreads / kInLanes, kInLoads = TOK / kInRows;
   static constexpr uint32_t kPieces = kOutLoads + kInLoads, kSlices = TOK / 16 * kPlanes;
   static constexpr uint32_t kM = kWaveOut / 32, kN = kWaveIn / 32;                               // products of 32 x 32 of a wave
   static_assert(kOutStride % 256 % 128 == 64 && kInStride % 256 % 128 == 64 && kOutRows * kOutLoads == TOK && kInRows * kInLoads == TOK && kSlices % 2 == 0 && TOK / 16 % 2 == 0, "");
@@ -117,7 +118,7 @@ __device__ __forceinline__ uint64_t column(uint64_t outs, uint64_t o0, uint32_t 
 // What a lane has on its way from memory: its part of a step.
 template <typename T, typename S>
 struct Stage {
-  a32x4 dy[S::kOutLoads * (__is_same(T, F32) ? 2 : 1)], x[S::kInLoads];
+  a32x4 dy[S::kOutLoads * (__is_same(T, F32) ? 2 : 1)], x[S::kInLoads];  // (8 codes: the first half)
   uint32_t scale[S::kInLoads];
 };
 
@@ -139,7 +140,7 @@ struct Walker {
 
   __device__ __forceinline__ Walker(const WGrad &g_, uint32_t lds)
       : g(g_), base(lds), wave(threadIdx.x >> 6), out_row(threadIdx.x / S::kOutLanes), out_col(threadIdx.x % S::kOutLanes * 8),
-        in_row(threadIdx.x / S::kInLanes), in_col(threadIdx.x % S::kInLanes * 16) {
+        in_row(threadIdx.x / S::kInLanes), in_col(threadIdx.x % S::kInLanes * S::kCodes) {
     put_dy = base + out_row * S::kOutStride + out_col * 2;
     put_x = base + S::kX + in_row * S::kInStride + in_col * 2;
     get_dy = base + (wave & 1u) * (S::kWaveOut * 2) + read_at(S::kOutStride);
@@ -201,7 +202,12 @@ struct Walker {
       uint64_t ahead = j * S::kInRows;
       const uint64_t t = first + (uint64_t)step * S::kTok + in_row;
       if (LAST && t + ahead >= end) ahead = end - 1 - t;
-      st.x[j] = a_ld<a32x4>(codes + ahead * g.pitch);
+      if constexpr (S::kCodes == 16) {
+        st.x[j] = a_ld<a32x4>(codes + ahead * g.pitch);
+      } else {
+        const a32x2 c = a_ld<a32x2>(codes + ahead * g.pitch);
+        st.x[j] = a32x4{c.x, c.y, 0u, 0u};
+      }
       st.scale[j] = a_ld<uint8_t>(scales + ahead * (g.pitch / kCkptBlock));
     }
   }
@@ -256,12 +262,12 @@ struct Walker {
       const float X = a_float(st.scale[j] << 23);
       a32x4 w[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < (int)S::kCodes / 4; ++i) {
         w[i / 2][i % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(st.x[j][i], X, false));
         w[i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(st.x[j][i], X, true));
       }
       *reinterpret_cast<lds_a32x4 *>(at) = w[0];
-      *reinterpret_cast<lds_a32x4 *>(at + 16) = w[1];
+      if constexpr (S::kCodes == 16) *reinterpret_cast<lds_a32x4 *>(at + 16) = w[1];
     }
   }
   // A step is kSlices rounds of kM x kN products: 16 tokens, and of a binary32 dy one of its three parts.
@@ -381,14 +387,17 @@ struct Walker {
     }
   }
   __device__ __forceinline__ void put_part(uint64_t unit) {
+    const uint64_t o = o0 + (wave & 1u) * S::kWaveOut, i = i0 + (wave >> 1) * S::kWaveIn;
     float *p = g.part + (unit * (S::kThreads / 64) + wave) * (uint64_t)(S::kM * S::kN * 1024) + (threadIdx.x & 63u) * 4;
 #pragma unroll
     for (uint32_t m = 0; m < S::kM; ++m)
 #pragma unroll
-      for (uint32_t n = 0; n < S::kN; ++n)
+      for (uint32_t n = 0; n < S::kN; ++n) {
+        if (o + m * 32 >= g.outs || i + n * 32 >= g.cols) continue;  // nobody reads them
 #pragma unroll
         for (uint32_t q = 0; q < 4; ++q)
           a_st<af32x4>(p + ((m * S::kN + n) * 4 + q) * 256, af32x4{acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]});
+      }
   }
   // The lanes of a column, through LDS.
   __device__ __forceinline__ void put_bias(uint64_t units, uint32_t split) {
@@ -431,28 +440,55 @@ __global__ __launch_bounds__(S::kThreads) void k_wgrad(WGrad g) {
   }
 }
 
-// The splits' sums, in their order.  A thread has four of a tile, as a lane of the kernel above had them.
-template <typename O, typename S, bool SMALL>
+// The splits' sums.  A thread has four of a tile, as a lane of the kernel above had them; where splits are many, WAYS threads share them,
+// each every WAYS-th, and their sums are added in order.
+template <typename O, typename S, bool SMALL, uint32_t WAYS>
 __global__ __launch_bounds__(kJoinThreads) void k_wgrad_join(WGrad g) {
   constexpr uint64_t kQuads = S::kOut * S::kIn / 4;
+  constexpr uint32_t kEach = kJoinThreads / WAYS;
+  __shared__ af32x4 lds[WAYS > 1 ? kJoinThreads : 1];
+  const uint32_t way = threadIdx.x / kEach;
   const uint64_t quads = g.tiles * kQuads, all = quads + (g.db ? g.outs : 0);
-  for (uint64_t i = (uint64_t)blockIdx.x * kJoinThreads + threadIdx.x; i < all; i += (uint64_t)gridDim.x * kJoinThreads) {
+  for (uint64_t first = (uint64_t)blockIdx.x * kEach; first < all; first += (uint64_t)gridDim.x * kEach) {
+    const uint64_t i = first + threadIdx.x % kEach;
+    af32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    uint64_t o0 = 0, at = 0;
+    uint32_t row = 0;
+    bool here = i < all;
     if (i < quads) {
-      af32x4 v = a_ld<af32x4>(g.part + i * 4);
-      for (uint32_t s = 1; s < g.splits; ++s) v += a_ld<af32x4>(g.part + (s * quads + i) * 4);
       const uint64_t tile = i / kQuads;
       const uint32_t k = (uint32_t)(i % kQuads), l = k & 63u, q = (k >> 6) & 3u, mn = (k >> 8) % (S::kM * S::kN), wave = (k >> 8) / (S::kM * S::kN);
-      const uint32_t row = (wave & 1u) * S::kWaveOut + mn / S::kN * 32 + 8 * q + 4 * (l >> 5), col = (wave >> 1) * S::kWaveIn + mn % S::kN * 32 + (l & 31u);
+      const uint32_t patch = (wave & 1u) * S::kWaveOut + mn / S::kN * 32;
+      o0 = tile_out(g, tile) * S::kOut;
+      row = patch + 8 * q + 4 * (l >> 5);
+      at = tile_in(g, tile) * S::kIn + (wave >> 1) * S::kWaveIn + mn % S::kN * 32 + (l & 31u);
+      here = o0 + patch < g.outs && at < g.cols;
+      if (here) {
+#pragma unroll 4
+        for (uint32_t s = way; s < g.splits; s += WAYS) v += a_ld<af32x4>(g.part + (s * quads + i) * 4);
+      }
+    } else if (here) {
+      const float *p = g.part + g.splits * quads * 4 + (i - quads);
+#pragma unroll 4
+      for (uint32_t s = way; s < g.splits; s += WAYS) v[0] += a_ld<float>(p + s * g.outs);
+    }
+    if constexpr (WAYS > 1) {
+      __syncthreads();  // the last sums have been read
+      lds[threadIdx.x] = v;
+      __syncthreads();
+      if (way) continue;
+#pragma unroll
+      for (uint32_t w = 1; w < WAYS; ++w) v += lds[w * kEach + threadIdx.x];
+    }
+    if (!here) continue;
+    if (i < quads) {
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) {
-        const uint64_t o = column<SMALL>(g.outs, tile_out(g, tile) * S::kOut, row + r), i = tile_in(g, tile) * S::kIn + col;
-        if (o < g.outs && i < g.cols) put<O>(g.dw, o * g.ld + i, v[r], g.accumulate);
+        const uint64_t o = column<SMALL>(g.outs, o0, row + r);
+        if (o < g.outs) put<O>(g.dw, o * g.ld + at, v[r], g.accumulate);
       }
     } else {
-      const float *p = g.part + g.splits * quads * 4 + (i - quads);
-      float v = 0.0f;
-      for (uint32_t s = 0; s < g.splits; ++s) v += a_ld<float>(p + s * g.outs);
-      put<O>(g.db, i - quads, v, g.accumulate);
+      put<O>(g.db, i - quads, v[0], g.accumulate);
     }
   }
 }
@@ -463,26 +499,44 @@ struct Cut {
   uint32_t splits;
   uint64_t tiles_out, tiles_in, split_rows;
 };
-constexpr uint32_t kEdges[3] = {64, 128, 256}, kToks[2][3] = {{64, 32, 32}, {64, 64, 64}};  // [bf16][size]
+constexpr uint32_t kEdges[3] = {64, 128, 256}, kToks[2][3] = {{32, 32, 32}, {64, 64, 64}};  // [bf16][size]
+constexpr uint32_t kManySplits = 16;                                                       // of which several threads join one sum
 
+// The cut that costs least, by what was measured (MI355X, microseconds): a step of a block alone on its CU and of one among as many as
+// fit, the launch, and what splits add, a launch and their sums' way to memory and back at 5 TB/s.  Large tiles read and move
+// least for what they multiply; small ones and splits give every CU a part where sums are few.
 Cut cut_of(dq_dtype dtype, uint64_t rows, uint64_t outs, uint64_t cols) {
-  const uint64_t cus = 256;
-  Cut c;
-  c.size = 2;
-  if (outs < 8) c.size = 0;
-  while (c.size > 0 && ((outs + kEdges[c.size] - 1) / kEdges[c.size] * ((cols + kEdges[c.size] - 1) / kEdges[c.size])) < 64) --c.size;
-  const uint32_t e = kEdges[c.size], tok = kToks[dtype == DQ_BF16][c.size];
-  c.tiles_out = (outs + e - 1) / e;
-  c.tiles_in = (cols + e - 1) / e;
-  const uint64_t tiles = c.tiles_out * c.tiles_in, steps = (rows + tok - 1) / tok;
-  uint64_t splits = tiles >= cus ? 1 : cus / tiles;
-  if (splits > steps / 4) splits = steps / 4;
-  if (splits < 1) splits = 1;
-  const uint64_t each = (steps + splits - 1) / splits;
-  c.splits = each ? (uint32_t)((steps + each - 1) / each) : 1u;
-  if (c.splits < 1) c.splits = 1;
-  c.split_rows = each * tok;
-  return c;
+  constexpr uint64_t kCus = 256;
+  struct Cost { uint32_t fit; double alone, among; };  // blocks on a CU, a step's time
+  static constexpr Cost kCosts[2][3] = {{{3, 0.35, 0.78}, {2, 0.76, 1.39}, {1, 2.3, 2.3}}, {{3, 0.36, 0.79}, {2, 0.70, 1.12}, {1, 1.75, 1.75}}};
+  Cut best = {};
+  double least = 0;
+  for (uint32_t size = 0; size < (outs < 8 ? 1u : 3u); ++size) {
+    const Cost &cost = kCosts[dtype == DQ_BF16][size];
+    const uint64_t e = kEdges[size], tok = kToks[dtype == DQ_BF16][size], steps = (rows + tok - 1) / tok;
+    Cut c = {size, 1, (outs + e - 1) / e, (cols + e - 1) / e, steps * tok};
+    const uint64_t tiles = c.tiles_out * c.tiles_in;
+    for (uint64_t k = 0; k <= 2 * cost.fit; ++k) {  // one split, or as many as make up to k units for every CU
+      uint64_t splits = 1;
+      if (k) {
+        splits = k * kCus / tiles < steps / 4 ? k * kCus / tiles : steps / 4;
+        if (splits <= 1) continue;
+      }
+      const uint64_t each = steps ? (steps + splits - 1) / splits : 1;
+      if (steps) splits = (steps + each - 1) / each;
+      const uint64_t on_cu = (tiles * splits + kCus - 1) / kCus, rest = on_cu % cost.fit;
+      double us = 3 + (double)each * ((double)(on_cu / cost.fit) * cost.among +
+                                      (rest ? cost.alone + (cost.among - cost.alone) * (double)(rest - 1) / (cost.fit > 1 ? cost.fit - 1 : 1) : 0.0));
+      if (splits > 1) us += 3 + (double)(splits * tiles * e * e) * 8 / 5.0e6;
+      if ((size == 0 && k == 0) || us < least) {
+        least = us;
+        best = c;
+        best.splits = (uint32_t)splits;
+        best.split_rows = each * tok;
+      }
+    }
+  }
+  return best;
 }
 
 bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -493,8 +547,12 @@ hipError_t run(const WGrad &g, hipStream_t s) {
   hipLaunchKernelGGL((k_wgrad<T, O, S, SMALL>), dim3((uint32_t)(units < 65536 ? units : 65536)), dim3(S::kThreads), 0, s, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.splits == 1) return e;
-  const uint64_t blocks = (g.tiles * (S::kOut * S::kIn / 4) + (g.db ? g.outs : 0) + kJoinThreads - 1) / kJoinThreads;
-  hipLaunchKernelGGL((k_wgrad_join<O, S, SMALL>), dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(kJoinThreads), 0, s, g);
+  const uint64_t all = g.tiles * (S::kOut * S::kIn / 4) + (g.db ? g.outs : 0);
+  constexpr uint32_t kWays = 8;
+  const uint64_t per_block = g.splits < kManySplits ? kJoinThreads : kJoinThreads / kWays, blocks = (all + per_block - 1) / per_block;
+  const dim3 grid((uint32_t)(blocks < 65536 ? blocks : 65536));
+  if (g.splits < kManySplits) hipLaunchKernelGGL((k_wgrad_join<O, S, SMALL, 1>), grid, dim3(kJoinThreads), 0, s, g);
+  else hipLaunchKernelGGL((k_wgrad_join<O, S, SMALL, kWays>), grid, dim3(kJoinThreads), 0, s, g);
   return hipGetLastError();
 }
 template <typename T, typename O>
