@@ -37,20 +37,132 @@ struct NormIn {
   Rows x;
   uint64_t rows, cols;
   const void *weight, *bias;  // or null: ones, zeros
+  uint32_t bf16;              // whether they are bf16
   float eps;
 };
-template <typename W>
-__device__ __forceinline__ void weight8(const void *w, uint64_t col, uint64_t cols, float otherwise, float (&v)[8]) {
+__device__ __forceinline__ void weight8(const void *w, uint32_t bf16, uint64_t col, uint64_t cols, float otherwise, float (&v)[8]) {
   if (w) {
-    load8<W>(w, col, cols, v);
+    if (bf16) load8<Bf16>(w, col, cols, v);
+    else load8<F32>(w, col, cols, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = otherwise;
   }
 }
 
-// A block per row, which it reads three times (the second and third time from the cache).
-template <typename T, typename W>
+// Rows of up to 16,384 entries stay in registers: GROUP threads have one, KEEP chunks of 8 each, and read it once.  A row goes to one
+// wave where that is enough (up to 2,048 entries) and there are rows for all, so that its sums need no barrier.
+//
+// A block's groups take a row each, the block then the next rows; all of them come round as often as each other.
+template <uint32_t GROUP, uint32_t KEEP>
+struct Fit {
+  static constexpr uint32_t kGroup = GROUP, kKeep = KEEP;
+  static constexpr bool kHold = GROUP < 1024;  // whether weights stay in registers too, of which 1,024 threads have 128 each
+  static constexpr uint32_t kBlock = GROUP < 512 ? 512 : GROUP, kGroups = kBlock / GROUP;  // of the backward pass
+};
+// Sums of a and b over a group, in all its threads; the order is fixed.  All threads of the block come here.
+template <uint32_t GROUP>
+__device__ __forceinline__ void group_sums(float &a, float &b, af32x2 *lds) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    a += __shfl_xor(a, d);
+    b += __shfl_xor(b, d);
+  }
+  if constexpr (GROUP > 64) {
+    const uint32_t wave = threadIdx.x >> 6, first = wave / (GROUP / 64) * (GROUP / 64);
+    __syncthreads();  // the last sums have been read
+    if ((threadIdx.x & 63u) == 0) lds[wave] = af32x2{a, b};
+    __syncthreads();
+    a = b = 0.0f;
+#pragma unroll
+    for (uint32_t i = 0; i < GROUP / 64; ++i) {
+      const af32x2 v = lds[first + i];
+      a += v.x;
+      b += v.y;
+    }
+  }
+}
+
+template <typename T, typename F>
+__global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(NormIn in, Rows y, CkptOut saved, float *mean, float *rstd) {
+  constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
+  __shared__ af32x2 lds[kBlock / 64];
+  const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, cols = (uint32_t)in.cols;
+  const float inv = 1.0f / (float)in.cols;
+  float w[F::kHold ? F::kKeep : 1][8], b[F::kHold ? F::kKeep : 1][8];
+  if constexpr (F::kHold) {
+#pragma unroll
+    for (uint32_t k = 0; k < F::kKeep; ++k) {
+      weight8(in.weight, in.bf16, (me + k * F::kGroup) * 8, cols, 1.0f, w[k]);
+      weight8(in.bias, in.bf16, (me + k * F::kGroup) * 8, cols, 0.0f, b[k]);
+    }
+  }
+  for (uint64_t first = (uint64_t)blockIdx.x * kGroups; first < in.rows; first += (uint64_t)gridDim.x * kGroups) {
+    const uint64_t r = first + threadIdx.x / F::kGroup;
+    const bool here = r < in.rows;
+    const uint8_t *x = static_cast<const uint8_t *>(in.x.data) + r * in.x.ld * kEntry<T>;
+    float v[F::kKeep][8], s = 0.0f, none = 0.0f;
+#pragma unroll
+    for (uint32_t k = 0; k < F::kKeep; ++k) {
+      const uint32_t c = me + k * F::kGroup;
+      if (here && c < chunks) {
+        load8<T>(x, c * 8, cols, v[k]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[k][i] = 0.0f;
+      }
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < F::kKeep; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[k][i];
+    group_sums<F::kGroup>(s, none, lds);
+    const float m = s * inv;
+    s = none = 0.0f;
+#pragma unroll
+    for (uint32_t k = 0; k < F::kKeep; ++k) {
+      int left = (int)cols - (int)((me + k * F::kGroup) * 8);  // of the row from this chunk on
+      asm volatile("" : "+v"(left));                            // (compared here, not in front of the loop, which would take 64 masks)
+      if (left >= 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float d = v[k][i] - m;
+          s = fmaf(d, d, s);
+        }
+      } else if (left > 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float d = i < left ? v[k][i] - m : 0.0f;
+          s = fmaf(d, d, s);
+        }
+      }
+    }
+    group_sums<F::kGroup>(s, none, lds);
+    if (!here) continue;
+    const float scale = 1.0f / sqrtf(fmaf(s, inv, in.eps));
+#pragma unroll
+    for (uint32_t k = 0; k < F::kKeep; ++k) {
+      const uint32_t c = me + k * F::kGroup;
+      if (c >= chunks) continue;
+      if (saved.codes) ckpt_store8(saved, r * chunks + c, v[k]);
+      if constexpr (!F::kHold) {
+        weight8(in.weight, in.bf16, c * 8, cols, 1.0f, w[0]);
+        weight8(in.bias, in.bf16, c * 8, cols, 0.0f, b[0]);
+      }
+      constexpr uint32_t kHeld = F::kHold ? 1 : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[k][i] = fmaf((v[k][i] - m) * scale, w[k * kHeld][i], b[k * kHeld][i]);
+      store8<T>(static_cast<uint8_t *>(y.data) + r * y.ld * kEntry<T>, c * 8, cols, v[k]);
+    }
+    if (me == 0 && mean) {
+      mean[r] = m;
+      rstd[r] = scale;
+    }
+  }
+}
+
+// Longer rows: a block per row, which it reads three times (the second and third time from the cache).
+template <typename T>
 __global__ __launch_bounds__(kThreads) void k_norm_wide(NormIn in, Rows y, CkptOut saved, float *mean, float *rstd) {
   __shared__ float lds[2 * kThreads / 64];
   const uint64_t chunks = ckpt_pitch(in.cols) / 8;
@@ -80,8 +192,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_wide(NormIn in, Rows y, CkptO
       float w[8], b[8];
       load8<T>(x, c * 8, in.cols, v);
       if (saved.codes) ckpt_store8(saved, r * chunks + c, v);
-      weight8<W>(in.weight, c * 8, in.cols, 1.0f, w);
-      weight8<W>(in.bias, c * 8, in.cols, 0.0f, b);
+      weight8(in.weight, in.bf16, c * 8, in.cols, 1.0f, w);
+      weight8(in.bias, in.bf16, c * 8, in.cols, 0.0f, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = fmaf((v[i] - m) * k, w[i], b[i]);
       store8<T>(static_cast<uint8_t *>(y.data) + r * y.ld * kEntry<T>, c * 8, in.cols, v);
@@ -99,8 +211,106 @@ struct NormGrad {
   CkptIn x;
   const float *mean, *rstd;
   const void *weight;
+  uint32_t bf16;
 };
-template <typename T, typename W>
+
+// The backward pass of rows that stay in registers, with the sums over rows beside: a thread's columns are the same in all of its
+// rows, so it sums them up as they pass; at the end the block's groups add up in turn and the block's sums go to `part`
+// ([blocks][2][pitch]).  One block of 512 threads to a CU (8 waves have what it takes in flight), so that there are few.
+template <typename T, typename F>
+__global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *part) {
+  __shared__ af32x2 lds[F::kBlock / 64];
+  __shared__ __attribute__((aligned(16))) float sums[F::kGroups > 1 ? F::kGroup * F::kKeep * 16 : 4];
+  const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, group = threadIdx.x / F::kGroup, cols = (uint32_t)in.cols;
+  const float inv = 1.0f / (float)in.cols;
+  float w[F::kHold ? F::kKeep : 1][8], dw[F::kKeep][8], db[F::kKeep][8];
+#pragma unroll
+  for (uint32_t k = 0; k < F::kKeep; ++k) {
+    if constexpr (F::kHold) weight8(in.weight, in.bf16, (me + k * F::kGroup) * 8, cols, 1.0f, w[k]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dw[k][i] = db[k][i] = 0.0f;
+  }
+  for (uint64_t first = (uint64_t)blockIdx.x * F::kGroups; first < in.rows; first += (uint64_t)gridDim.x * F::kGroups) {
+    const uint64_t r = first + group;
+    const bool here = r < in.rows;
+    float g[F::kKeep][8], n[F::kKeep][8], s = 0.0f, sn = 0.0f, m = 0.0f, scale = 0.0f;
+    if (here) {
+      m = a_ld<float>(in.mean + r);
+      scale = a_ld<float>(in.rstd + r);
+    }
+    const uint8_t *dy = static_cast<const uint8_t *>(in.dy.data) + r * in.dy.ld * kEntry<T>;
+#pragma unroll
+    for (uint32_t k = 0; k < F::kKeep; ++k) {
+      const uint32_t c = me + k * F::kGroup;
+      if (here && c < chunks) {
+        load8<T>(dy, c * 8, cols, g[k]);
+        ckpt_load8(in.x, r * chunks + c, n[k]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[k][i] = n[k][i] = 0.0f;
+      }
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < F::kKeep; ++k) {
+      if constexpr (!F::kHold) weight8(in.weight, in.bf16, (me + k * F::kGroup) * 8, cols, 1.0f, w[0]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        n[k][i] = (n[k][i] - m) * scale;
+        dw[k][i] = fmaf(g[k][i], n[k][i], dw[k][i]);
+        db[k][i] += g[k][i];
+        g[k][i] *= w[F::kHold ? k : 0][i];
+        s += g[k][i];
+        sn = fmaf(g[k][i], n[k][i], sn);
+      }
+    }
+    group_sums<F::kGroup>(s, sn, lds);
+    if (!here) continue;
+    s *= inv;
+    sn *= inv;
+#pragma unroll
+    for (uint32_t k = 0; k < F::kKeep; ++k) {
+      const uint32_t c = me + k * F::kGroup;
+      if (c >= chunks) continue;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[k][i] = scale * ((g[k][i] - s) - n[k][i] * sn);
+      store8<T>(static_cast<uint8_t *>(in.dx.data) + r * in.dx.ld * kEntry<T>, c * 8, cols, g[k]);
+    }
+  }
+  if (!part) return;
+  float *out = part + (uint64_t)blockIdx.x * 2 * chunks * 8;
+  for (uint32_t turn = 0; turn < F::kGroups; ++turn) {
+    if (group == turn) {
+#pragma unroll
+      for (uint32_t k = 0; k < F::kKeep; ++k) {
+        const uint32_t c = me + k * F::kGroup;
+        if (c >= chunks) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float *at = sums + (k * F::kGroup + me) * 4 + h * F::kGroup * F::kKeep * 4;  // (16 bytes a lane: no bank is asked twice)
+          af32x4 a = {dw[k][4 * h], dw[k][4 * h + 1], dw[k][4 * h + 2], dw[k][4 * h + 3]}, b = {db[k][4 * h], db[k][4 * h + 1], db[k][4 * h + 2], db[k][4 * h + 3]};
+          constexpr uint32_t kDb = F::kGroup * F::kKeep * 8;
+          if constexpr (F::kGroups > 1) {
+            if (turn) {
+              a += *reinterpret_cast<af32x4 *>(at);
+              b += *reinterpret_cast<af32x4 *>(at + kDb);
+            }
+            if (turn + 1 < F::kGroups) {
+              *reinterpret_cast<af32x4 *>(at) = a;
+              *reinterpret_cast<af32x4 *>(at + kDb) = b;
+              continue;
+            }
+          }
+          a_st<af32x4>(out + c * 8 + 4 * h, a);
+          a_st<af32x4>(out + chunks * 8 + c * 8 + 4 * h, b);
+        }
+      }
+    }
+    if constexpr (F::kGroups > 1) __syncthreads();
+  }
+}
+
+// Longer rows, in two kernels.
+template <typename T>
 __global__ __launch_bounds__(kThreads) void k_norm_grad_wide(NormGrad in) {
   __shared__ float lds[2 * kThreads / 64];
   const uint64_t chunks = ckpt_pitch(in.cols) / 8;
@@ -112,7 +322,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_wide(NormGrad in) {
     for (uint64_t c = threadIdx.x; c < chunks; c += kThreads) {
       load8<T>(dy, c * 8, in.cols, q);  // zero behind the row's end
       ckpt_load8(in.x, r * chunks + c, x);
-      weight8<W>(in.weight, c * 8, in.cols, 1.0f, w);
+      weight8(in.weight, in.bf16, c * 8, in.cols, 1.0f, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         q[i] *= w[i];
@@ -126,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_wide(NormGrad in) {
     for (uint64_t c = threadIdx.x; c < chunks; c += kThreads) {
       load8<T>(dy, c * 8, in.cols, q);
       ckpt_load8(in.x, r * chunks + c, x);
-      weight8<W>(in.weight, c * 8, in.cols, 1.0f, w);
+      weight8(in.weight, in.bf16, c * 8, in.cols, 1.0f, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) q[i] = k * (fmaf(q[i], w[i], -s) - (x[i] - m) * k * sn);
       store8<T>(static_cast<uint8_t *>(in.dx.data) + r * in.dx.ld * kEntry<T>, c * 8, in.cols, q);
@@ -192,8 +402,67 @@ __global__ __launch_bounds__(kJoinThreads) void k_norm_join(const float *part, u
 
 constexpr uint32_t kRowBlocks = 2048;  // blocks that rows are dealt to
 uint32_t row_blocks(uint64_t rows) { return (uint32_t)(rows < kRowBlocks ? rows : kRowBlocks); }
-// Slices of the rows for the sums over them.
-uint32_t norm_slices(uint64_t rows) { return (uint32_t)(rows < 256 * 8 ? (rows + 7) / 8 : 256); }
+
+// How rows are kept: threads to a row and chunks to a thread (group 0: the row is too long).
+struct Kept {
+  uint32_t group, keep;
+};
+Kept kept(uint64_t rows, uint64_t cols) {
+  const uint64_t chunks = ckpt_pitch(cols) / 8;
+  // a wave to a row, unless there are fewer rows than make two waves for every SIMD: then four
+  uint32_t group = chunks <= 64 ? 64 : chunks <= 256 ? (rows < 2048 ? 256 : 64) : chunks <= 1024 ? 256 : 1024;
+  uint32_t keep = 1;
+  while (keep < (group == 1024 ? 2 : 4) && (uint64_t)group * keep < chunks) keep *= 2;
+  if ((uint64_t)group * keep < chunks) group = 0;
+  return {group, keep};
+}
+// Parts of the sums over rows: blocks of the backward pass (Fit::kGroups rows at a time), or slices of the rows.
+uint32_t norm_parts(uint64_t rows, uint64_t cols) {
+  const Kept k = kept(rows, cols);
+  const uint64_t at_once = k.group == 0 ? 8 : k.group < 512 ? 512 / k.group : 1, parts = (rows + at_once - 1) / at_once;
+  return (uint32_t)(parts < 256 ? parts : 256);
+}
+template <typename T, typename F>
+hipError_t run_norm(const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
+  constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
+  const uint64_t blocks = (in.rows + kGroups - 1) / kGroups, most = 256 * (1024 / kBlock);
+  hipLaunchKernelGGL((k_norm<T, F>), dim3((uint32_t)(blocks < most ? blocks : most)), dim3(kBlock), 0, s, in, y, saved, mean, rstd);
+  return hipGetLastError();
+}
+template <typename T, typename F>
+hipError_t run_norm_grad(const NormGrad &in, float *part, uint32_t parts, hipStream_t s) {
+  hipLaunchKernelGGL((k_norm_grad<T, F>), dim3(parts), dim3(F::kBlock), 0, s, in, part);
+  return hipGetLastError();
+}
+#define DQ_FITS(run, ...)                                       \
+  switch (k.group * 8 + k.keep) {                               \
+    case 64 * 8 + 1: return run<T, Fit<64, 1>>(__VA_ARGS__);    \
+    case 64 * 8 + 2: return run<T, Fit<64, 2>>(__VA_ARGS__);    \
+    case 64 * 8 + 4: return run<T, Fit<64, 4>>(__VA_ARGS__);    \
+    case 256 * 8 + 1: return run<T, Fit<256, 1>>(__VA_ARGS__);  \
+    case 256 * 8 + 2: return run<T, Fit<256, 2>>(__VA_ARGS__);  \
+    case 256 * 8 + 4: return run<T, Fit<256, 4>>(__VA_ARGS__);  \
+    case 1024 * 8 + 2: return run<T, Fit<1024, 2>>(__VA_ARGS__); \
+  }
+template <typename T>
+hipError_t norm_forward(const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
+  const Kept k = kept(in.rows, in.cols);
+  DQ_FITS(run_norm, in, y, saved, mean, rstd, s)
+  hipLaunchKernelGGL((k_norm_wide<T>), dim3(row_blocks(in.rows)), dim3(kThreads), 0, s, in, y, saved, mean, rstd);
+  return hipGetLastError();
+}
+// part: null if nobody wants the sums over rows.
+template <typename T>
+hipError_t norm_backward(const NormGrad &in, float *part, uint32_t parts, hipStream_t s) {
+  const Kept k = kept(in.rows, in.cols);
+  DQ_FITS(run_norm_grad, in, part, parts, s)
+  hipLaunchKernelGGL((k_norm_grad_wide<T>), dim3(row_blocks(in.rows)), dim3(kThreads), 0, s, in);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !part) return e;
+  const dim3 grid((uint32_t)((ckpt_pitch(in.cols) / 8 + kThreads - 1) / kThreads), parts);
+  hipLaunchKernelGGL((k_norm_columns<T>), grid, dim3(kThreads), 0, s, in, (in.rows + parts - 1) / parts, part);
+  return hipGetLastError();
+}
 
 uint32_t join_grid(uint64_t pitch) { return (uint32_t)(2 * pitch / kJoinCols < 4096 ? 2 * pitch / kJoinCols : 4096); }
 
@@ -227,20 +496,16 @@ dq_status dq_layer_norm(const dq_matrix *x, uint64_t rows, uint64_t cols, const 
   const Region r[] = {region(x, rows, cols, false), region(weight, cols * wb, false), region(bias, cols * wb, false), region(y, rows, cols, true),
                       region(ckpt, bytes, true), region(mean, rows * 4, true), region(rstd, rows * 4, true)};
   if (regions_meet(r, 7)) return DQ_EINVAL;
-  const NormIn in = {{x->data, x->ld}, rows, cols, weight, bias, eps};
+  const NormIn in = {{x->data, x->ld}, rows, cols, weight, bias, (uint32_t)(weight_dtype == DQ_BF16), eps};
   const Rows out = {y->data, y->ld};
   const CkptOut saved = ckpt_out(ckpt, rows, cols);
-#define DQ_NORM(T, W) hipLaunchKernelGGL((k_norm_wide<T, W>), dim3(row_blocks(rows)), dim3(kThreads), 0, (hipStream_t)hip_stream, in, out, saved, mean, rstd)
-  if (x->dtype == DQ_F32 && weight_dtype == DQ_F32) DQ_NORM(F32, F32);
-  else if (x->dtype == DQ_F32) DQ_NORM(F32, Bf16);
-  else if (weight_dtype == DQ_F32) DQ_NORM(Bf16, F32);
-  else DQ_NORM(Bf16, Bf16);
-  return hip_status(hipGetLastError());
+  hipStream_t s = (hipStream_t)hip_stream;
+  return hip_status(x->dtype == DQ_F32 ? norm_forward<F32>(in, out, saved, mean, rstd, s) : norm_forward<Bf16>(in, out, saved, mean, rstd, s));
 }
 
 size_t dq_layer_norm_grad_scratch_bytes(uint64_t rows, uint64_t cols) {
   if (dq_ckpt_bytes(rows, cols) == 0 || cols >> 31) return 0;
-  return (size_t)norm_slices(rows) * 2 * ckpt_pitch(cols) * 4;
+  return (size_t)norm_parts(rows, cols) * 2 * ckpt_pitch(cols) * 4;
 }
 
 dq_status dq_layer_norm_grad(const dq_matrix *dy, const void *ckpt, const float *mean, const float *rstd, uint64_t rows, uint64_t cols,
@@ -260,7 +525,7 @@ dq_status dq_layer_norm_grad(const dq_matrix *dy, const void *ckpt, const float 
   }
   const size_t bytes = rows ? dq_ckpt_bytes(rows, cols) : 0, need = dq_layer_norm_grad_scratch_bytes(rows, cols);
   const uint64_t pitch = ckpt_pitch(cols);
-  const uint32_t slices = norm_slices(rows), join_blocks = join_grid(pitch);
+  const uint32_t parts = rows ? norm_parts(rows, cols) : 0, join_blocks = join_grid(pitch);
   hipStream_t s = (hipStream_t)hip_stream;
   if (rows) {
     if (bytes == 0) return DQ_EUNSUPPORTED;
@@ -271,25 +536,16 @@ dq_status dq_layer_norm_grad(const dq_matrix *dy, const void *ckpt, const float 
                         region(rstd, rows * 4, false),      region(weight, cols * wb, false),   region(dx, rows, cols, true),
                         region(dweight, cols * wb, true),   region(dbias, cols * wb, true),     region(dweight ? scratch : nullptr, need, true)};
     if (regions_meet(r, 9)) return DQ_EINVAL;
-    const NormGrad in = {{dy->data, dy->ld}, {dx->data, dx->ld}, rows, cols, ckpt_in(ckpt, rows, cols), mean, rstd, weight};
-#define DQ_NORM_GRAD(T, W) hipLaunchKernelGGL((k_norm_grad_wide<T, W>), dim3(row_blocks(rows)), dim3(kThreads), 0, s, in)
-    if (dy->dtype == DQ_F32 && weight_dtype == DQ_F32) DQ_NORM_GRAD(F32, F32);
-    else if (dy->dtype == DQ_F32) DQ_NORM_GRAD(F32, Bf16);
-    else if (weight_dtype == DQ_F32) DQ_NORM_GRAD(Bf16, F32);
-    else DQ_NORM_GRAD(Bf16, Bf16);
-    DQ_TRY(hip_status(hipGetLastError()));
+    const NormGrad in = {{dy->data, dy->ld}, {dx->data, dx->ld}, rows, cols, ckpt_in(ckpt, rows, cols), mean, rstd, weight, (uint32_t)(weight_dtype == DQ_BF16)};
+    float *part = dweight ? static_cast<float *>(scratch) : nullptr;
+    DQ_TRY(hip_status(dy->dtype == DQ_F32 ? norm_backward<F32>(in, part, parts, s) : norm_backward<Bf16>(in, part, parts, s)));
     if (!dweight) return DQ_OK;
-    const dim3 grid((uint32_t)((pitch / 8 + kThreads - 1) / kThreads), slices);
-    const uint64_t slice_rows = (rows + slices - 1) / slices;
-    if (dy->dtype == DQ_F32) hipLaunchKernelGGL((k_norm_columns<F32>), grid, dim3(kThreads), 0, s, in, slice_rows, (float *)scratch);
-    else hipLaunchKernelGGL((k_norm_columns<Bf16>), grid, dim3(kThreads), 0, s, in, slice_rows, (float *)scratch);
-    DQ_TRY(hip_status(hipGetLastError()));
   }
   if (weight_dtype == DQ_F32)
-    hipLaunchKernelGGL((k_norm_join<F32>), dim3(join_blocks), dim3(kJoinThreads), 0, s, (const float *)scratch, pitch, cols, slices, dweight, dbias,
+    hipLaunchKernelGGL((k_norm_join<F32>), dim3(join_blocks), dim3(kJoinThreads), 0, s, (const float *)scratch, pitch, cols, parts, dweight, dbias,
                        (uint32_t)(accumulate != 0));
   else
-    hipLaunchKernelGGL((k_norm_join<Bf16>), dim3(join_blocks), dim3(kJoinThreads), 0, s, (const float *)scratch, pitch, cols, slices, dweight, dbias,
+    hipLaunchKernelGGL((k_norm_join<Bf16>), dim3(join_blocks), dim3(kJoinThreads), 0, s, (const float *)scratch, pitch, cols, parts, dweight, dbias,
                        (uint32_t)(accumulate != 0));
   return hip_status(hipGetLastError());
 }
