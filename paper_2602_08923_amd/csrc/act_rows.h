@@ -46,30 +46,50 @@ struct Bf16 {};
 template <typename T>
 constexpr uint32_t kEntry = __is_same(T, F32) ? 4 : 2;
 
+// Eight entries as they lie in memory.
+template <typename T>
+struct Raw8 {
+  a32x4 w[kEntry<T> / 2];
+};
 // Entries col .. col + 7 of the row at `row`, of which `cols` exist; the others are zero.
 template <typename T>
-__device__ __forceinline__ void load8(const void *row, uint64_t col, uint64_t cols, float (&v)[8]) {
+__device__ __forceinline__ Raw8<T> load_raw8(const void *row, uint64_t col, uint64_t cols) {
   const uint8_t *p = static_cast<const uint8_t *>(row) + col * kEntry<T>;
+  Raw8<T> r;
   if (col + 8 <= cols) {
-    if constexpr (__is_same(T, F32)) {
-      const af32x4 a = a_ld<af32x4_any>(p), b = a_ld<af32x4_any>(p + 16);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-    } else {
-      const a32x4 a = a_ld<a32x4_any>(p);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { v[2 * i] = a_float(a[i] << 16); v[2 * i + 1] = a_float(a[i] & 0xFFFF0000u); }
-    }
+    r.w[0] = a_ld<a32x4_any>(p);
+    if constexpr (__is_same(T, F32)) r.w[1] = a_ld<a32x4_any>(p + 16);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[i] = 0.0f;
-      if (col + i < cols) {
-        if constexpr (__is_same(T, F32)) v[i] = a_ld<float>(p + 4 * i);
-        else v[i] = a_float((uint32_t)a_ld<uint16_t>(p + 2 * i) << 16);
+    for (int i = 0; i < (int)kEntry<T> * 2; ++i) {
+      uint32_t v = 0;
+      if constexpr (__is_same(T, F32)) {
+        if (col + i < cols) v = a_ld<uint32_t>(p + 4 * i);
+      } else {
+        if (col + 2 * i < cols) v = a_ld<uint16_t>(p + 4 * i);
+        if (col + 2 * i + 1 < cols) v |= (uint32_t)a_ld<uint16_t>(p + 4 * i + 2) << 16;
       }
+      r.w[i / 4][i % 4] = v;
     }
   }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw8<T> &r, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (__is_same(T, F32)) {
+      v[i] = a_float(r.w[0][i]);
+      v[4 + i] = a_float(r.w[1][i]);
+    } else {
+      v[2 * i] = a_float(r.w[0][i] << 16);
+      v[2 * i + 1] = a_float(r.w[0][i] & 0xFFFF0000u);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void load8(const void *row, uint64_t col, uint64_t cols, float (&v)[8]) {
+  widen8<T>(load_raw8<T>(row, col, cols), v);
 }
 // Two binary32 numbers as bf16, rounded to nearest even.
 __device__ __forceinline__ uint32_t to_bf16x2(float a, float b) {

@@ -12,13 +12,26 @@ namespace {
 
 constexpr uint32_t kThreads = 256;
 
+// The sum over a wave, in all its lanes: within rows of 16 lanes by moves that the addition makes itself, then over the rows (a swap
+// of two copies' rows, or halves, leaves what is to be added in the two).  Through LDS, as shuffles go, a sum took 100 cycles a step.
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+  return v + a_float((uint32_t)__builtin_amdgcn_mov_dpp((int)a_bits(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v = add_dpp<0xB1>(v);   // lanes 1 0 3 2
+  v = add_dpp<0x4E>(v);   // lanes 2 3 0 1
+  v = add_dpp<0x141>(v);  // mirrored within 8
+  v = add_dpp<0x140>(v);  // mirrored within 16
+  const auto a = __builtin_amdgcn_permlane16_swap(a_bits(v), a_bits(v), false, false);
+  v = a_float(a[0]) + a_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(a_bits(v), a_bits(v), false, false);
+  return a_float(b[0]) + a_float(b[1]);
+}
 // Sums of a and b over the block, in every thread; the order is fixed.
 __device__ __forceinline__ void block_sums(float &a, float &b, float *lds) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    a += __shfl_xor(a, d);
-    b += __shfl_xor(b, d);
-  }
+  a = wave_sum(a);
+  b = wave_sum(b);
   const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   __syncthreads();  // the last row's sums have been read
   if ((threadIdx.x & 63u) == 0) {
@@ -57,17 +70,13 @@ __device__ __forceinline__ void weight8(const void *w, uint32_t bf16, uint64_t c
 template <uint32_t GROUP, uint32_t KEEP>
 struct Fit {
   static constexpr uint32_t kGroup = GROUP, kKeep = KEEP;
-  static constexpr bool kHold = GROUP < 1024;  // whether weights stay in registers too, of which 1,024 threads have 128 each
   static constexpr uint32_t kBlock = GROUP < 512 ? 512 : GROUP, kGroups = kBlock / GROUP;  // of the backward pass
 };
 // Sums of a and b over a group, in all its threads; the order is fixed.  All threads of the block come here.
 template <uint32_t GROUP>
 __device__ __forceinline__ void group_sums(float &a, float &b, af32x2 *lds) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    a += __shfl_xor(a, d);
-    b += __shfl_xor(b, d);
-  }
+  a = wave_sum(a);
+  b = wave_sum(b);
   if constexpr (GROUP > 64) {
     const uint32_t wave = threadIdx.x >> 6, first = wave / (GROUP / 64) * (GROUP / 64);
     __syncthreads();  // the last sums have been read
@@ -83,35 +92,75 @@ __device__ __forceinline__ void group_sums(float &a, float &b, af32x2 *lds) {
   }
 }
 
+// A weight (or a bias) as the threads of a group read it, eight entries at a time: where a wave has a row, from LDS, which leaves it
+// registers for the next row; else from registers, of which 1,024 threads have too few: they read it from memory each time.
+template <typename F>
+struct Weight {
+  float v[F::kGroup == 256 ? F::kKeep : 1][8];
+  const void *w;
+  uint32_t bf16, cols, lds;
+  float otherwise;
+  static constexpr uint32_t kLds = F::kGroup == 64 ? F::kKeep * 64 * 8 : 4;  // floats
+  __device__ __forceinline__ Weight(const void *w_, uint32_t bf16_, uint32_t cols_, float otherwise_, float *buffer)
+      : w(w_), bf16(bf16_), cols(cols_), lds((uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)buffer), otherwise(otherwise_) {
+    if constexpr (F::kGroup == 256) {
+#pragma unroll
+      for (uint32_t k = 0; k < F::kKeep; ++k) weight8(w, bf16, (threadIdx.x % 256 + k * 256) * 8, cols, otherwise, v[k]);
+    } else if constexpr (F::kGroup == 64) {  // the chunks' first halves, then their second ones: 16 bytes a lane, side by side
+      for (uint32_t c = threadIdx.x; c < F::kKeep * 64; c += blockDim.x) {
+        float u[8];
+        weight8(w, bf16, c * 8, cols, otherwise, u);
+        put(c, u[0], u[1], u[2], u[3]);
+        put(F::kKeep * 64 + c, u[4], u[5], u[6], u[7]);
+      }
+    }
+  }
+  typedef __attribute__((address_space(3))) af32x4 lds_quad;
+  __device__ __forceinline__ void put(uint32_t i, float a, float b, float c, float d) const { *reinterpret_cast<lds_quad *>(lds + i * 16) = af32x4{a, b, c, d}; }
+  __device__ __forceinline__ void get(uint32_t k, uint32_t chunk, float (&u)[8]) const {
+    if constexpr (F::kGroup == 64) {
+      const af32x4 a = *reinterpret_cast<const lds_quad *>(lds + chunk * 16), b = *reinterpret_cast<const lds_quad *>(lds + (F::kKeep * 64 + chunk) * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { u[i] = a[i]; u[4 + i] = b[i]; }
+    } else if constexpr (F::kGroup == 256) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = v[k][i];
+    } else {
+      weight8(w, bf16, chunk * 8, cols, otherwise, u);
+    }
+  }
+};
+
 template <typename T, typename F>
 __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(NormIn in, Rows y, CkptOut saved, float *mean, float *rstd) {
   constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
+  constexpr bool kAhead = F::kGroup == 64;  // a wave loads its next row while it works on one
   __shared__ af32x2 lds[kBlock / 64];
+  __shared__ __attribute__((aligned(16))) float weights[2][Weight<F>::kLds];
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, cols = (uint32_t)in.cols;
   const float inv = 1.0f / (float)in.cols;
-  float w[F::kHold ? F::kKeep : 1][8], b[F::kHold ? F::kKeep : 1][8];
-  if constexpr (F::kHold) {
-#pragma unroll
-    for (uint32_t k = 0; k < F::kKeep; ++k) {
-      weight8(in.weight, in.bf16, (me + k * F::kGroup) * 8, cols, 1.0f, w[k]);
-      weight8(in.bias, in.bf16, (me + k * F::kGroup) * 8, cols, 0.0f, b[k]);
-    }
-  }
-  for (uint64_t first = (uint64_t)blockIdx.x * kGroups; first < in.rows; first += (uint64_t)gridDim.x * kGroups) {
-    const uint64_t r = first + threadIdx.x / F::kGroup;
-    const bool here = r < in.rows;
+  const Weight<F> w(in.weight, in.bf16, cols, 1.0f, weights[0]), b(in.bias, in.bf16, cols, 0.0f, weights[1]);
+  if constexpr (F::kGroup == 64) __syncthreads();
+  Raw8<T> next[F::kKeep];
+  auto load = [&](uint64_t r) {
     const uint8_t *x = static_cast<const uint8_t *>(in.x.data) + r * in.x.ld * kEntry<T>;
-    float v[F::kKeep][8], s = 0.0f, none = 0.0f;
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
       const uint32_t c = me + k * F::kGroup;
-      if (here && c < chunks) {
-        load8<T>(x, c * 8, cols, v[k]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[k][i] = 0.0f;
-      }
+      next[k] = Raw8<T>{};
+      if (r < in.rows && c < chunks) next[k] = load_raw8<T>(x, c * 8, cols);
     }
+  };
+  const uint64_t step = (uint64_t)gridDim.x * kGroups;
+  uint64_t r = (uint64_t)blockIdx.x * kGroups + threadIdx.x / F::kGroup;
+  if (kAhead) load(r);
+  for (uint64_t first = (uint64_t)blockIdx.x * kGroups; first < in.rows; first += step, r += step) {
+    const bool here = r < in.rows;
+    if (!kAhead) load(r);
+    float v[F::kKeep][8], s = 0.0f, none = 0.0f;
+#pragma unroll
+    for (uint32_t k = 0; k < F::kKeep; ++k) widen8<T>(next[k], v[k]);
+    if (kAhead) load(r + step);
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k)
 #pragma unroll
@@ -145,13 +194,11 @@ __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(Norm
       const uint32_t c = me + k * F::kGroup;
       if (c >= chunks) continue;
       if (saved.codes) ckpt_store8(saved, r * chunks + c, v[k]);
-      if constexpr (!F::kHold) {
-        weight8(in.weight, in.bf16, c * 8, cols, 1.0f, w[0]);
-        weight8(in.bias, in.bf16, c * 8, cols, 0.0f, b[0]);
-      }
-      constexpr uint32_t kHeld = F::kHold ? 1 : 0;
+      float wk[8], bk[8];
+      w.get(k, c, wk);
+      b.get(k, c, bk);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[k][i] = fmaf((v[k][i] - m) * scale, w[k * kHeld][i], b[k * kHeld][i]);
+      for (int i = 0; i < 8; ++i) v[k][i] = fmaf((v[k][i] - m) * scale, wk[i], bk[i]);
       store8<T>(static_cast<uint8_t *>(y.data) + r * y.ld * kEntry<T>, c * 8, cols, v[k]);
     }
     if (me == 0 && mean) {
@@ -219,46 +266,67 @@ struct NormGrad {
 // ([blocks][2][pitch]).  One block of 512 threads to a CU (8 waves have what it takes in flight), so that there are few.
 template <typename T, typename F>
 __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *part) {
+  constexpr bool kAhead = F::kGroup == 64;  // a wave loads its next row while it works on one
   __shared__ af32x2 lds[F::kBlock / 64];
-  __shared__ __attribute__((aligned(16))) float sums[F::kGroups > 1 ? F::kGroup * F::kKeep * 16 : 4];
+  __shared__ __attribute__((aligned(16))) float weights[Weight<F>::kLds], sums[F::kGroups > 1 ? F::kGroup * F::kKeep * 16 : 4];
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, group = threadIdx.x / F::kGroup, cols = (uint32_t)in.cols;
   const float inv = 1.0f / (float)in.cols;
-  float w[F::kHold ? F::kKeep : 1][8], dw[F::kKeep][8], db[F::kKeep][8];
+  const Weight<F> w(in.weight, in.bf16, cols, 1.0f, weights);
+  if constexpr (F::kGroup == 64) __syncthreads();
+  float dw[F::kKeep][8], db[F::kKeep][8];
 #pragma unroll
-  for (uint32_t k = 0; k < F::kKeep; ++k) {
-    if constexpr (F::kHold) weight8(in.weight, in.bf16, (me + k * F::kGroup) * 8, cols, 1.0f, w[k]);
+  for (uint32_t k = 0; k < F::kKeep; ++k)
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[k][i] = db[k][i] = 0.0f;
-  }
-  for (uint64_t first = (uint64_t)blockIdx.x * F::kGroups; first < in.rows; first += (uint64_t)gridDim.x * F::kGroups) {
-    const uint64_t r = first + group;
+  Raw8<T> next[F::kKeep];
+  a32x2 codes[F::kKeep];
+  uint32_t scales[F::kKeep];
+  float next_m, next_scale;
+  auto load = [&](uint64_t r) {
     const bool here = r < in.rows;
-    float g[F::kKeep][8], n[F::kKeep][8], s = 0.0f, sn = 0.0f, m = 0.0f, scale = 0.0f;
+    next_m = next_scale = 0.0f;
     if (here) {
-      m = a_ld<float>(in.mean + r);
-      scale = a_ld<float>(in.rstd + r);
+      next_m = a_ld<float>(in.mean + r);
+      next_scale = a_ld<float>(in.rstd + r);
     }
     const uint8_t *dy = static_cast<const uint8_t *>(in.dy.data) + r * in.dy.ld * kEntry<T>;
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
       const uint32_t c = me + k * F::kGroup;
+      next[k] = Raw8<T>{};
+      codes[k] = a32x2{0u, 0u};
+      scales[k] = kCkptLeast;
       if (here && c < chunks) {
-        load8<T>(dy, c * 8, cols, g[k]);
-        ckpt_load8(in.x, r * chunks + c, n[k]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[k][i] = n[k][i] = 0.0f;
+        next[k] = load_raw8<T>(dy, c * 8, cols);
+        codes[k] = a_ld<a32x2>(in.x.codes + (r * chunks + c) * 8);
+        scales[k] = a_ld<uint8_t>(in.x.scales + (r * chunks + c) / 4);
       }
     }
+  };
+  const uint64_t step = (uint64_t)gridDim.x * F::kGroups;
+  uint64_t r = (uint64_t)blockIdx.x * F::kGroups + group;
+  if (kAhead) load(r);
+  for (uint64_t first = (uint64_t)blockIdx.x * F::kGroups; first < in.rows; first += step, r += step) {
+    const bool here = r < in.rows;
+    if (!kAhead) load(r);
+    float g[F::kKeep][8], n[F::kKeep][8], s = 0.0f, sn = 0.0f;
+    const float m = next_m, scale = next_scale;
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
-      if constexpr (!F::kHold) weight8(in.weight, in.bf16, (me + k * F::kGroup) * 8, cols, 1.0f, w[0]);
+      widen8<T>(next[k], g[k]);
+      ckpt_decode(codes[k], scales[k], n[k]);
+    }
+    if (kAhead) load(r + step);
+#pragma unroll
+    for (uint32_t k = 0; k < F::kKeep; ++k) {
+      float wk[8];
+      w.get(k, me + k * F::kGroup, wk);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         n[k][i] = (n[k][i] - m) * scale;
         dw[k][i] = fmaf(g[k][i], n[k][i], dw[k][i]);
         db[k][i] += g[k][i];
-        g[k][i] *= w[F::kHold ? k : 0][i];
+        g[k][i] *= wk[i];
         s += g[k][i];
         sn = fmaf(g[k][i], n[k][i], sn);
       }
@@ -425,7 +493,7 @@ uint32_t norm_parts(uint64_t rows, uint64_t cols) {
 template <typename T, typename F>
 hipError_t run_norm(const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
   constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
-  const uint64_t blocks = (in.rows + kGroups - 1) / kGroups, most = 256 * (1024 / kBlock);
+  const uint64_t blocks = (in.rows + kGroups - 1) / kGroups, most = 256 * (F::kGroup == 64 ? 4 : 1024 / kBlock);
   hipLaunchKernelGGL((k_norm<T, F>), dim3((uint32_t)(blocks < most ? blocks : most)), dim3(kBlock), 0, s, in, y, saved, mean, rstd);
   return hipGetLastError();
 }
