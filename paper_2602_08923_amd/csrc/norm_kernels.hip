@@ -70,6 +70,7 @@ __device__ __forceinline__ void weight8(const void *w, uint32_t bf16, uint64_t c
 template <uint32_t GROUP, uint32_t KEEP>
 struct Fit {
   static constexpr uint32_t kGroup = GROUP, kKeep = KEEP;
+  static constexpr bool kAhead = GROUP == 64 || (GROUP == 256 && KEEP <= 3);  // the next row is loaded while one is worked on
   static constexpr uint32_t kBlock = GROUP < 512 ? 512 : GROUP, kGroups = kBlock / GROUP;  // of the backward pass
 };
 // Sums of a and b over a group, in all its threads; the order is fixed.  All threads of the block come here.
@@ -134,7 +135,7 @@ struct Weight {
 template <typename T, typename F>
 __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(NormIn in, Rows y, CkptOut saved, float *mean, float *rstd) {
   constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
-  constexpr bool kAhead = F::kGroup == 64;  // a wave loads its next row while it works on one
+  constexpr bool kAhead = F::kAhead;
   __shared__ af32x2 lds[kBlock / 64];
   __shared__ __attribute__((aligned(16))) float weights[2][Weight<F>::kLds];
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, cols = (uint32_t)in.cols;
@@ -266,7 +267,7 @@ struct NormGrad {
 // ([blocks][2][pitch]).  One block of 512 threads to a CU (8 waves have what it takes in flight), so that there are few.
 template <typename T, typename F>
 __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *part) {
-  constexpr bool kAhead = F::kGroup == 64;  // a wave loads its next row while it works on one
+  constexpr bool kAhead = F::kAhead;
   __shared__ af32x2 lds[F::kBlock / 64];
   __shared__ __attribute__((aligned(16))) float weights[Weight<F>::kLds], sums[F::kGroups > 1 ? F::kGroup * F::kKeep * 16 : 4];
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, group = threadIdx.x / F::kGroup, cols = (uint32_t)in.cols;
@@ -480,7 +481,7 @@ Kept kept(uint64_t rows, uint64_t cols) {
   // a wave to a row, unless there are fewer rows than make two waves for every SIMD: then four
   uint32_t group = chunks <= 64 ? 64 : chunks <= 256 ? (rows < 2048 ? 256 : 64) : chunks <= 1024 ? 256 : 1024;
   uint32_t keep = 1;
-  while (keep < (group == 1024 ? 2 : 4) && (uint64_t)group * keep < chunks) keep *= 2;
+  while (keep < (group == 1024 ? 2 : 4) && (uint64_t)group * keep < chunks) keep += group == 64 && keep == 2 ? 2 : 1;
   if ((uint64_t)group * keep < chunks) group = 0;
   return {group, keep};
 }
@@ -493,7 +494,7 @@ uint32_t norm_parts(uint64_t rows, uint64_t cols) {
 template <typename T, typename F>
 hipError_t run_norm(const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
   constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
-  const uint64_t blocks = (in.rows + kGroups - 1) / kGroups, most = 256 * (F::kGroup == 64 ? 4 : 1024 / kBlock);
+  const uint64_t blocks = (in.rows + kGroups - 1) / kGroups, most = 256 * (kBlock == 256 ? 4 : 1);
   hipLaunchKernelGGL((k_norm<T, F>), dim3((uint32_t)(blocks < most ? blocks : most)), dim3(kBlock), 0, s, in, y, saved, mean, rstd);
   return hipGetLastError();
 }
@@ -509,6 +510,7 @@ hipError_t run_norm_grad(const NormGrad &in, float *part, uint32_t parts, hipStr
     case 64 * 8 + 4: return run<T, Fit<64, 4>>(__VA_ARGS__);    \
     case 256 * 8 + 1: return run<T, Fit<256, 1>>(__VA_ARGS__);  \
     case 256 * 8 + 2: return run<T, Fit<256, 2>>(__VA_ARGS__);  \
+    case 256 * 8 + 3: return run<T, Fit<256, 3>>(__VA_ARGS__);  \
     case 256 * 8 + 4: return run<T, Fit<256, 4>>(__VA_ARGS__);  \
     case 1024 * 8 + 2: return run<T, Fit<1024, 2>>(__VA_ARGS__); \
   }
