@@ -70,7 +70,8 @@ __device__ __forceinline__ void weight8(const void *w, uint32_t bf16, uint64_t c
 template <uint32_t GROUP, uint32_t KEEP>
 struct Fit {
   static constexpr uint32_t kGroup = GROUP, kKeep = KEEP;
-  static constexpr bool kAhead = GROUP == 64 || (GROUP == 256 && KEEP <= 3);  // the next row is loaded while one is worked on
+  // whether the next row is loaded while one is worked on: where the registers last for it
+  static constexpr bool kAheadForward = GROUP < 1024, kAheadBackward = GROUP == 64 || (GROUP < 1024 && KEEP <= 3);
   static constexpr uint32_t kBlock = GROUP < 512 ? 512 : GROUP, kGroups = kBlock / GROUP;  // of the backward pass
 };
 // Sums of a and b over a group, in all its threads; the order is fixed.  All threads of the block come here.
@@ -97,16 +98,17 @@ __device__ __forceinline__ void group_sums(float &a, float &b, af32x2 *lds) {
 // registers for the next row; else from registers, of which 1,024 threads have too few: they read it from memory each time.
 template <typename F>
 struct Weight {
-  float v[F::kGroup == 256 ? F::kKeep : 1][8];
+  static constexpr bool kHeld = F::kGroup == 128 || F::kGroup == 256;
+  float v[kHeld ? F::kKeep : 1][8];
   const void *w;
   uint32_t bf16, cols, lds;
   float otherwise;
   static constexpr uint32_t kLds = F::kGroup == 64 ? F::kKeep * 64 * 8 : 4;  // floats
   __device__ __forceinline__ Weight(const void *w_, uint32_t bf16_, uint32_t cols_, float otherwise_, float *buffer)
       : w(w_), bf16(bf16_), cols(cols_), lds((uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)buffer), otherwise(otherwise_) {
-    if constexpr (F::kGroup == 256) {
+    if constexpr (kHeld) {
 #pragma unroll
-      for (uint32_t k = 0; k < F::kKeep; ++k) weight8(w, bf16, (threadIdx.x % 256 + k * 256) * 8, cols, otherwise, v[k]);
+      for (uint32_t k = 0; k < F::kKeep; ++k) weight8(w, bf16, (threadIdx.x % F::kGroup + k * F::kGroup) * 8, cols, otherwise, v[k]);
     } else if constexpr (F::kGroup == 64) {  // the chunks' first halves, then their second ones: 16 bytes a lane, side by side
       for (uint32_t c = threadIdx.x; c < F::kKeep * 64; c += blockDim.x) {
         float u[8];
@@ -123,7 +125,7 @@ struct Weight {
       const af32x4 a = *reinterpret_cast<const lds_quad *>(lds + chunk * 16), b = *reinterpret_cast<const lds_quad *>(lds + (F::kKeep * 64 + chunk) * 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) { u[i] = a[i]; u[4 + i] = b[i]; }
-    } else if constexpr (F::kGroup == 256) {
+    } else if constexpr (kHeld) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) u[i] = v[k][i];
     } else {
@@ -135,7 +137,7 @@ struct Weight {
 template <typename T, typename F>
 __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(NormIn in, Rows y, CkptOut saved, float *mean, float *rstd) {
   constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
-  constexpr bool kAhead = F::kAhead;
+  constexpr bool kAhead = F::kAheadForward;
   __shared__ af32x2 lds[kBlock / 64];
   __shared__ __attribute__((aligned(16))) float weights[2][Weight<F>::kLds];
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, cols = (uint32_t)in.cols;
@@ -267,7 +269,7 @@ struct NormGrad {
 // ([blocks][2][pitch]).  One block of 512 threads to a CU (8 waves have what it takes in flight), so that there are few.
 template <typename T, typename F>
 __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *part) {
-  constexpr bool kAhead = F::kAhead;
+  constexpr bool kAhead = F::kAheadBackward;
   __shared__ af32x2 lds[F::kBlock / 64];
   __shared__ __attribute__((aligned(16))) float weights[Weight<F>::kLds], sums[F::kGroups > 1 ? F::kGroup * F::kKeep * 16 : 4];
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, group = threadIdx.x / F::kGroup, cols = (uint32_t)in.cols;
@@ -479,8 +481,8 @@ struct Kept {
 Kept kept(uint64_t rows, uint64_t cols) {
   const uint64_t chunks = ckpt_pitch(cols) / 8;
   // a wave to a row, unless there are fewer rows than make two waves for every SIMD: then four
-  uint32_t group = chunks <= 64 ? 64 : chunks <= 256 ? (rows < 2048 ? 256 : 64) : chunks <= 1024 ? 256 : 1024;
-  uint32_t keep = 1;
+  uint32_t group = chunks <= 64 ? 64 : chunks <= 256 ? (rows < 2048 ? 256 : 64) : chunks <= 384 && rows >= 2048 ? 128 : chunks <= 1024 ? 256 : 1024;
+  uint32_t keep = group == 128 ? 3 : 1;
   while (keep < (group == 1024 ? 2 : 4) && (uint64_t)group * keep < chunks) keep += group == 64 && keep == 2 ? 2 : 1;
   if ((uint64_t)group * keep < chunks) group = 0;
   return {group, keep};
@@ -508,6 +510,7 @@ hipError_t run_norm_grad(const NormGrad &in, float *part, uint32_t parts, hipStr
     case 64 * 8 + 1: return run<T, Fit<64, 1>>(__VA_ARGS__);    \
     case 64 * 8 + 2: return run<T, Fit<64, 2>>(__VA_ARGS__);    \
     case 64 * 8 + 4: return run<T, Fit<64, 4>>(__VA_ARGS__);    \
+    case 128 * 8 + 3: return run<T, Fit<128, 3>>(__VA_ARGS__);  \
     case 256 * 8 + 1: return run<T, Fit<256, 1>>(__VA_ARGS__);  \
     case 256 * 8 + 2: return run<T, Fit<256, 2>>(__VA_ARGS__);  \
     case 256 * 8 + 3: return run<T, Fit<256, 3>>(__VA_ARGS__);  \
