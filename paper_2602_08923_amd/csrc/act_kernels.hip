@@ -12,6 +12,67 @@ namespace {
 
 constexpr uint32_t kMapThreads = 256;
 
+// Here a lane's chunk is 16 bytes of a row, so that a wave's loads and stores each cover memory without gaps: 8 entries of bf16, 4 of
+// binary32 (with 8 of them, 32 bytes, half of each line a store touched came with the next one: 16384 x 4096, saved and loaded, took 174 us, not 146).
+template <typename T>
+constexpr uint32_t kChunk = 16 / kEntry<T>;
+template <typename T>
+struct Chunk {
+  float v[kChunk<T>];
+};
+template <typename T>
+__device__ __forceinline__ Chunk<T> load_chunk(const void *row, uint64_t at, uint64_t cols) {
+  Chunk<T> c;
+  const uint64_t col = at * kChunk<T>;
+  if constexpr (__is_same(T, F32)) {
+    const uint8_t *p = static_cast<const uint8_t *>(row) + col * 4;
+    if (col + 4 <= cols) {
+      const af32x4 q = a_ld<af32x4_any>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c.v[i] = q[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c.v[i] = col + i < cols ? a_ld<float>(p + 4 * i) : 0.0f;
+    }
+  } else {
+    load8<T>(row, col, cols, c.v);
+  }
+  return c;
+}
+template <typename T>
+__device__ __forceinline__ void store_chunk(void *row, uint64_t at, uint64_t cols, const Chunk<T> &c) {
+  const uint64_t col = at * kChunk<T>;
+  if constexpr (__is_same(T, F32)) {
+    uint8_t *p = static_cast<uint8_t *>(row) + col * 4;
+    if (col + 4 <= cols) {
+      a_st<af32x4_any>(p, af32x4{c.v[0], c.v[1], c.v[2], c.v[3]});
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (col + i < cols) a_st<float>(p + 4 * i, c.v[i]);
+    }
+  } else {
+    store8<T>(row, col, cols, c.v);
+  }
+}
+// Chunk number n of a checkpoint.
+template <typename T>
+__device__ __forceinline__ void save_chunk(const CkptOut &out, uint64_t n, const Chunk<T> &c) {
+  constexpr uint32_t lanes = kCkptBlock / kChunk<T>;
+  uint32_t scale;
+  auto codes = ckpt_encode(c.v, &scale);
+  a_st<decltype(codes)>(out.codes + n * kChunk<T>, codes);
+  if (n % lanes == 0) a_st<uint8_t>(out.scales + n / lanes, (uint8_t)scale);
+}
+template <typename T>
+__device__ __forceinline__ Chunk<T> saved_chunk(const CkptIn &in, uint64_t n) {
+  Chunk<T> c;
+  const uint32_t scale = a_ld<uint8_t>(in.scales + n / (kCkptBlock / kChunk<T>));
+  if constexpr (__is_same(T, F32)) ckpt_decode(a_ld<uint32_t>(in.codes + n * 4), scale, c.v);
+  else ckpt_decode(a_ld<a32x2>(in.codes + n * 8), scale, c.v);
+  return c;
+}
+
 // The chunks of a matrix, in order, dealt to the threads; rows that lie back to back are one long row (the host sees to it).
 struct Walk8 {
   uint64_t chunks;             // in all
@@ -49,17 +110,13 @@ __device__ __forceinline__ uint8_t *row_of(const Rows &m, uint64_t row) {
 template <typename T>
 __global__ __launch_bounds__(kMapThreads) void k_ckpt_save(Walk8 w, Rows x, CkptOut out) {
   for (At i(w); i.chunk < w.chunks; i.next(w)) {
-    float v[8];
-    load8<T>(row_of<T>(x, i.row), i.at * 8, w.cols, v);
-    ckpt_store8(out, i.chunk, v);
+    save_chunk<T>(out, i.chunk, load_chunk<T>(row_of<T>(x, i.row), i.at, w.cols));
   }
 }
 template <typename T>
 __global__ __launch_bounds__(kMapThreads) void k_ckpt_load(Walk8 w, CkptIn in, Rows x) {
   for (At i(w); i.chunk < w.chunks; i.next(w)) {
-    float v[8];
-    ckpt_load8(in, i.chunk, v);
-    store8<T>(row_of<T>(x, i.row), i.at * 8, w.cols, v);
+    store_chunk<T>(row_of<T>(x, i.row), i.at, w.cols, saved_chunk<T>(in, i.chunk));
   }
 }
 
@@ -97,39 +154,38 @@ __device__ __forceinline__ void activation(float z, float *a, float *d) {
 template <typename T, int KIND, bool GATED, bool SAVE>
 __global__ __launch_bounds__(kMapThreads) void k_gate(Walk8 w, Rows z, Rows u, Rows h, CkptOut sz, CkptOut su) {
   for (At i(w); i.chunk < w.chunks; i.next(w)) {
-    float a[8], b[8], d;
-    load8<T>(row_of<T>(z, i.row), i.at * 8, w.cols, a);
-    if constexpr (GATED) load8<T>(row_of<T>(u, i.row), i.at * 8, w.cols, b);
-    if constexpr (SAVE) ckpt_store8(sz, i.chunk, a);
-    if constexpr (SAVE && GATED) ckpt_store8(su, i.chunk, b);
+    Chunk<T> a = load_chunk<T>(row_of<T>(z, i.row), i.at, w.cols), b;
+    if constexpr (GATED) b = load_chunk<T>(row_of<T>(u, i.row), i.at, w.cols);
+    if constexpr (SAVE) save_chunk<T>(sz, i.chunk, a);
+    if constexpr (SAVE && GATED) save_chunk<T>(su, i.chunk, b);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      activation<KIND>(a[k], &a[k], &d);
-      if constexpr (GATED) a[k] *= b[k];
+    for (uint32_t k = 0; k < kChunk<T>; ++k) {
+      float d;
+      activation<KIND>(a.v[k], &a.v[k], &d);
+      if constexpr (GATED) a.v[k] *= b.v[k];
     }
-    store8<T>(row_of<T>(h, i.row), i.at * 8, w.cols, a);
+    store_chunk<T>(row_of<T>(h, i.row), i.at, w.cols, a);
   }
 }
 template <typename T, int KIND, bool GATED>
 __global__ __launch_bounds__(kMapThreads) void k_gate_grad(Walk8 w, Rows dh, CkptIn sz, CkptIn su, Rows dz, Rows du) {
   for (At i(w); i.chunk < w.chunks; i.next(w)) {
-    float g[8], a[8], b[8];
-    load8<T>(row_of<T>(dh, i.row), i.at * 8, w.cols, g);
-    ckpt_load8(sz, i.chunk, a);
-    if constexpr (GATED) ckpt_load8(su, i.chunk, b);
+    const Chunk<T> g = load_chunk<T>(row_of<T>(dh, i.row), i.at, w.cols);
+    Chunk<T> a = saved_chunk<T>(sz, i.chunk), b;
+    if constexpr (GATED) b = saved_chunk<T>(su, i.chunk);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (uint32_t k = 0; k < kChunk<T>; ++k) {
       float act, d;
-      activation<KIND>(a[k], &act, &d);
+      activation<KIND>(a.v[k], &act, &d);
       if constexpr (GATED) {
-        a[k] = g[k] * b[k] * d;
-        b[k] = g[k] * act;
+        a.v[k] = g.v[k] * b.v[k] * d;
+        b.v[k] = g.v[k] * act;
       } else {
-        a[k] = g[k] * d;
+        a.v[k] = g.v[k] * d;
       }
     }
-    store8<T>(row_of<T>(dz, i.row), i.at * 8, w.cols, a);
-    if constexpr (GATED) store8<T>(row_of<T>(du, i.row), i.at * 8, w.cols, b);
+    store_chunk<T>(row_of<T>(dz, i.row), i.at, w.cols, a);
+    if constexpr (GATED) store_chunk<T>(row_of<T>(du, i.row), i.at, w.cols, b);
   }
 }
 
@@ -146,7 +202,7 @@ Map plan_map(uint64_t rows, uint64_t cols, std::initializer_list<const dq_matrix
     rows = 1;
   }
   Map p;
-  p.walk.per_row = ckpt_pitch(cols) / 8;
+  p.walk.per_row = ckpt_pitch(cols) * entry_bytes((*m.begin())->dtype) / 16;
   p.walk.chunks = rows * p.walk.per_row;
   p.walk.cols = cols;
   const uint64_t want = (p.walk.chunks + kMapThreads - 1) / kMapThreads, most = (uint64_t)device_cu_count() * 8;

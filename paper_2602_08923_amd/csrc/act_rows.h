@@ -124,29 +124,26 @@ __device__ __forceinline__ uint32_t block_max(uint32_t m) {
   m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xF, 0xF, true));   // lanes 1 0 3 2
   return max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xF, 0xF, true));  // lanes 2 3 0 1
 }
-// A lane's 8 entries of a block as codes, and the block's scale byte.  All four lanes of the block call it.  The scaled conversions
-// take the scale's exponent field; the narrowing one makes NaN of what is too large, so values are clamped first (448 is the largest).
+// Four codes of a block whose largest magnitude has the exponent field `top`, and the block's scale byte.  The scaled conversions take
+// the scale's exponent field; the narrowing one makes NaN of what is too large, so values are clamped first (448 is the largest).
+__device__ __forceinline__ uint32_t ckpt_codes(float a, float b, float c, float d, uint32_t top, uint32_t *scale) {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  const uint32_t e = max(top, kCkptLeast + 8) - 8;
+  const float X = a_float(e << 23), most = 448.0f * X;
+  s16x2 r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, __builtin_amdgcn_fmed3f(a, -most, most), __builtin_amdgcn_fmed3f(b, -most, most), X, false);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, __builtin_amdgcn_fmed3f(c, -most, most), __builtin_amdgcn_fmed3f(d, -most, most), X, true);
+  *scale = top == 255 ? 255u : e;
+  return top == 255 ? 0x7F7F7F7Fu : __builtin_bit_cast(uint32_t, r);
+}
+// A lane's 8 entries of a block as codes.  All four lanes of the block call it.
 __device__ __forceinline__ a32x2 ckpt_encode(const float (&v)[8], uint32_t *scale) {
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, a_bits(v[i]) & 0x7FFFFFFFu);
-  const uint32_t top = block_max(m) >> 23;
-  const uint32_t e = max(top, kCkptLeast + 8) - 8;
-  const float X = a_float(e << 23), most = 448.0f * X;
-  a32x2 codes;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    typedef short s16x2 __attribute__((ext_vector_type(2)));
-    float w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_fmed3f(v[4 * h + i], -most, most);
-    s16x2 r = {0, 0};
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, w[0], w[1], X, false);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, w[2], w[3], X, true);
-    codes[h] = top == 255 ? 0x7F7F7F7Fu : __builtin_bit_cast(uint32_t, r);
-  }
-  *scale = top == 255 ? 255u : e;
-  return codes;
+  m = block_max(m) >> 23;
+  const uint32_t lo = ckpt_codes(v[0], v[1], v[2], v[3], m, scale), hi = ckpt_codes(v[4], v[5], v[6], v[7], m, scale);
+  return a32x2{lo, hi};
 }
 __device__ __forceinline__ void ckpt_decode(a32x2 codes, uint32_t scale, float (&v)[8]) {
   const float X = a_float(scale << 23);
@@ -156,6 +153,20 @@ __device__ __forceinline__ void ckpt_decode(a32x2 codes, uint32_t scale, float (
     const af32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes[h], X, true);
     v[4 * h] = lo.x; v[4 * h + 1] = lo.y; v[4 * h + 2] = hi.x; v[4 * h + 3] = hi.y;
   }
+}
+// The same with four entries of binary32 a lane, eight lanes to a block.
+__device__ __forceinline__ uint32_t ckpt_encode(const float (&v)[4], uint32_t *scale) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = max(m, a_bits(v[i]) & 0x7FFFFFFFu);
+  m = block_max(m);
+  m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x141, 0xF, 0xF, true));  // mirrored within 8 lanes
+  return ckpt_codes(v[0], v[1], v[2], v[3], m >> 23, scale);
+}
+__device__ __forceinline__ void ckpt_decode(uint32_t codes, uint32_t scale, float (&v)[4]) {
+  const float X = a_float(scale << 23);
+  const af32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, X, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, X, true);
+  v[0] = lo.x; v[1] = lo.y; v[2] = hi.x; v[3] = hi.y;
 }
 // Chunk number `chunk` of a checkpoint (its rows back to back, each pitch / 8 chunks): codes at 8 * chunk, its block's scale behind them.
 struct CkptIn {
