@@ -7,6 +7,9 @@ off in this library, so that row of the paper's table has no counterpart here.
 
 With --scalability: the error against the worker count (Section 6.1: ring all-reduce, n = 2 .. 64),
 DynamiQ at 5 bits beside the three MX formats, on the same synthetic workload.
+
+With --block: the same rows on gradients that a backward pass leaves (block.py: a feed-forward block whose activations wait in 8-bit
+checkpoints), beside the error that the checkpoints themselves leave in a worker's gradients.
 """
 import argparse
 import json
@@ -15,7 +18,7 @@ import torch
 
 from . import allreduce as A
 from . import binding as B
-from . import workloads
+from . import block, workloads
 
 
 def main():
@@ -24,6 +27,9 @@ def main():
     ap.add_argument("--sg", type=int, default=8192)
     ap.add_argument("--topology", choices=["ring", "butterfly"], default="ring")
     ap.add_argument("--scalability", action="store_true", help="error against the worker count instead")
+    ap.add_argument("--block", action="store_true", help="gradients from a backward pass instead of synthetic ones")
+    ap.add_argument("--width", type=int, default=1024, help="of the block (--block); its inner width is twice that")
+    ap.add_argument("--tokens", type=int, default=4096, help="of a worker's micro-batch (--block)")
     args = ap.parse_args()
     dev = torch.device("cuda:0")
     n, J = args.workers, args.sg
@@ -33,12 +39,18 @@ def main():
     # every super-group at 4 bits costs 4 + 0.5 + 1/16 + 1/8 = 4.6875 bits per coordinate: the budget of all rows
     bits = 4.6875
     out = {}
-    for name, grads in (
-        ("lognormal-mixture magnitudes, Gaussian entries",
-         [workloads.draw_mixture(workloads.mixture_magnitudes(J, seed=2, device=dev), w, seed=2) for w in range(n)]),
-        ("lognormal-mixture magnitudes, 0.1 % of the entries x100",
-         [_with_outliers(workloads.draw_mixture(workloads.mixture_magnitudes(J, seed=2, device=dev), w, seed=2), w) for w in range(n)]),
-    ):
+    if args.block:
+        grads, lost = block.worker_gradients(block.Block(args.width, 2 * args.width, seed=2, device=dev), n, args.tokens, seed=2)
+        J = grads[0].numel() // block.S
+        sets = (("gradients of a feed-forward block", grads),)
+    else:
+        sets = (
+            ("lognormal-mixture magnitudes, Gaussian entries",
+             [workloads.draw_mixture(workloads.mixture_magnitudes(J, seed=2, device=dev), w, seed=2) for w in range(n)]),
+            ("lognormal-mixture magnitudes, 0.1 % of the entries x100",
+             [_with_outliers(workloads.draw_mixture(workloads.mixture_magnitudes(J, seed=2, device=dev), w, seed=2), w) for w in range(n)]),
+        )
+    for name, grads in sets:
         truth = A.true_sum(grads)
         rows = {}
         kw = dict(topology=topo, seed=5)
@@ -50,7 +62,10 @@ def main():
             A.simulated_allreduce(grads, bits, independent_rounding=True, **kw)[0], truth)
         rows["+ correlated rounding"] = A.vnmse(A.simulated_allreduce(grads, bits, **kw)[0], truth)
         out[name] = rows
-    print(json.dumps({"workers": n, "super_groups": J, "topology": args.topology, "budget_bits": bits, "vNMSE": out}, indent=1))
+    told = {"workers": n, "super_groups": J, "topology": args.topology, "budget_bits": bits, "vNMSE": out}
+    if args.block:
+        told["vNMSE_of_8_bit_checkpoints"] = lost
+    print(json.dumps(told, indent=1))
 
 
 def scalability(J, topo, topo_name, dev):
