@@ -323,7 +323,7 @@ struct Walker {
 #pragma unroll
     for (uint32_t i = 0; i < S::kM * S::kN; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS reads
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);  // LDS reads
       __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);  // vector arithmetic
       __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);  // LDS writes
       __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // loads
