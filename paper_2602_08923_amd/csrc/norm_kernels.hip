@@ -10,7 +10,7 @@
 namespace dq {
 namespace {
 
-constexpr uint32_t kThreads = 256;
+constexpr uint32_t kWideThreads = 1024, kThreads = 256;
 
 // The sum over a wave, in all its lanes: within rows of 16 lanes by moves that the addition makes itself, then over the rows (a swap
 // of two copies' rows, or halves, leaves what is to be added in the two).  Through LDS, as shuffles go, a sum took 100 cycles a step.
@@ -213,14 +213,14 @@ __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(Norm
 
 // Longer rows: a block per row, which it reads three times (the second and third time from the cache).
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_norm_wide(NormIn in, Rows y, CkptOut saved, float *mean, float *rstd) {
-  __shared__ float lds[2 * kThreads / 64];
+__global__ __launch_bounds__(kWideThreads) void k_norm_wide(NormIn in, Rows y, CkptOut saved, float *mean, float *rstd) {
+  __shared__ float lds[2 * kWideThreads / 64];
   const uint64_t chunks = ckpt_pitch(in.cols) / 8;
   const float inv = 1.0f / (float)in.cols;
   for (uint64_t r = blockIdx.x; r < in.rows; r += gridDim.x) {
     const uint8_t *x = static_cast<const uint8_t *>(in.x.data) + r * in.x.ld * kEntry<T>;
     float v[8], s = 0.0f, s2 = 0.0f;
-    for (uint64_t c = threadIdx.x; c < chunks; c += kThreads) {
+    for (uint64_t c = threadIdx.x; c < chunks; c += kWideThreads) {
       load8<T>(x, c * 8, in.cols, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += v[i];
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_wide(NormIn in, Rows y, CkptO
     block_sums(s, s2, lds);
     const float m = s * inv;
     s = s2 = 0.0f;
-    for (uint64_t c = threadIdx.x; c < chunks; c += kThreads) {
+    for (uint64_t c = threadIdx.x; c < chunks; c += kWideThreads) {
       load8<T>(x, c * 8, in.cols, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_wide(NormIn in, Rows y, CkptO
     }
     block_sums(s, s2, lds);
     const float k = 1.0f / sqrtf(fmaf(s, inv, in.eps));
-    for (uint64_t c = threadIdx.x; c < chunks; c += kThreads) {
+    for (uint64_t c = threadIdx.x; c < chunks; c += kWideThreads) {
       float w[8], b[8];
       load8<T>(x, c * 8, in.cols, v);
       if (saved.codes) ckpt_store8(saved, r * chunks + c, v);
@@ -382,15 +382,15 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
 
 // Longer rows, in two kernels.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_norm_grad_wide(NormGrad in) {
-  __shared__ float lds[2 * kThreads / 64];
+__global__ __launch_bounds__(kWideThreads) void k_norm_grad_wide(NormGrad in) {
+  __shared__ float lds[2 * kWideThreads / 64];
   const uint64_t chunks = ckpt_pitch(in.cols) / 8;
   const float inv = 1.0f / (float)in.cols;
   for (uint64_t r = blockIdx.x; r < in.rows; r += gridDim.x) {
     const uint8_t *dy = static_cast<const uint8_t *>(in.dy.data) + r * in.dy.ld * kEntry<T>;
     const float m = in.mean[r], k = in.rstd[r];
     float x[8], q[8], w[8], s = 0.0f, sn = 0.0f;
-    for (uint64_t c = threadIdx.x; c < chunks; c += kThreads) {
+    for (uint64_t c = threadIdx.x; c < chunks; c += kWideThreads) {
       load8<T>(dy, c * 8, in.cols, q);  // zero behind the row's end
       ckpt_load8(in.x, r * chunks + c, x);
       weight8(in.weight, in.bf16, c * 8, in.cols, 1.0f, w);
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_wide(NormGrad in) {
     block_sums(s, sn, lds);
     s *= inv;
     sn *= inv;
-    for (uint64_t c = threadIdx.x; c < chunks; c += kThreads) {
+    for (uint64_t c = threadIdx.x; c < chunks; c += kWideThreads) {
       load8<T>(dy, c * 8, in.cols, q);
       ckpt_load8(in.x, r * chunks + c, x);
       weight8(in.weight, in.bf16, c * 8, in.cols, 1.0f, w);
@@ -471,7 +471,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_norm_join(const float *part, u
   }
 }
 
-constexpr uint32_t kRowBlocks = 2048;  // blocks that rows are dealt to
+constexpr uint32_t kRowBlocks = 512;  // blocks that longer rows are dealt to
 uint32_t row_blocks(uint64_t rows) { return (uint32_t)(rows < kRowBlocks ? rows : kRowBlocks); }
 
 // How rows are kept: threads to a row and chunks to a thread (group 0: the row is too long).
@@ -521,7 +521,7 @@ template <typename T>
 hipError_t norm_forward(const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
   const Kept k = kept(in.rows, in.cols);
   DQ_FITS(run_norm, in, y, saved, mean, rstd, s)
-  hipLaunchKernelGGL((k_norm_wide<T>), dim3(row_blocks(in.rows)), dim3(kThreads), 0, s, in, y, saved, mean, rstd);
+  hipLaunchKernelGGL((k_norm_wide<T>), dim3(row_blocks(in.rows)), dim3(kWideThreads), 0, s, in, y, saved, mean, rstd);
   return hipGetLastError();
 }
 // part: null if nobody wants the sums over rows.
@@ -529,7 +529,7 @@ template <typename T>
 hipError_t norm_backward(const NormGrad &in, float *part, uint32_t parts, hipStream_t s) {
   const Kept k = kept(in.rows, in.cols);
   DQ_FITS(run_norm_grad, in, part, parts, s)
-  hipLaunchKernelGGL((k_norm_grad_wide<T>), dim3(row_blocks(in.rows)), dim3(kThreads), 0, s, in);
+  hipLaunchKernelGGL((k_norm_grad_wide<T>), dim3(row_blocks(in.rows)), dim3(kWideThreads), 0, s, in);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !part) return e;
   const dim3 grid((uint32_t)((ckpt_pitch(in.cols) / 8 + kThreads - 1) / kThreads), parts);
