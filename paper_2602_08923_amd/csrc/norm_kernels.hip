@@ -496,7 +496,7 @@ uint32_t norm_parts(uint64_t rows, uint64_t cols) {
 template <typename T, typename F>
 hipError_t run_norm(const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
   constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
-  const uint64_t blocks = (in.rows + kGroups - 1) / kGroups, most = 256 * (kBlock == 256 ? 4 : 1);
+  const uint64_t blocks = (in.rows + kGroups - 1) / kGroups, most = 256 * (kBlock > 256 ? 1 : F::kGroup == 256 && F::kKeep > 2 ? 6 - F::kKeep : 4);
   hipLaunchKernelGGL((k_norm<T, F>), dim3((uint32_t)(blocks < most ? blocks : most)), dim3(kBlock), 0, s, in, y, saved, mean, rstd);
   return hipGetLastError();
 }
