@@ -12,26 +12,32 @@ namespace {
 
 constexpr uint32_t kWideThreads = 1024, kThreads = 256;
 
-// The sum over a wave, in all its lanes: within rows of 16 lanes by moves that the addition makes itself, then over the rows (a swap
+// The sum over a wave, or over each 16 or 32 of its lanes, in all of them: within rows of 16 lanes by moves that the addition makes itself, then over the rows (a swap
 // of two copies' rows, or halves, leaves what is to be added in the two).  Through LDS, as shuffles go, a sum took 100 cycles a step.
 template <int CTRL>
 __device__ __forceinline__ float add_dpp(float v) {
   return v + a_float((uint32_t)__builtin_amdgcn_mov_dpp((int)a_bits(v), CTRL, 0xF, 0xF, true));
 }
-__device__ __forceinline__ float wave_sum(float v) {
+template <uint32_t LANES = 64>
+__device__ __forceinline__ float lanes_sum(float v) {
   v = add_dpp<0xB1>(v);   // lanes 1 0 3 2
   v = add_dpp<0x4E>(v);   // lanes 2 3 0 1
   v = add_dpp<0x141>(v);  // mirrored within 8
   v = add_dpp<0x140>(v);  // mirrored within 16
-  const auto a = __builtin_amdgcn_permlane16_swap(a_bits(v), a_bits(v), false, false);
-  v = a_float(a[0]) + a_float(a[1]);
-  const auto b = __builtin_amdgcn_permlane32_swap(a_bits(v), a_bits(v), false, false);
-  return a_float(b[0]) + a_float(b[1]);
+  if constexpr (LANES > 16) {
+    const auto a = __builtin_amdgcn_permlane16_swap(a_bits(v), a_bits(v), false, false);
+    v = a_float(a[0]) + a_float(a[1]);
+  }
+  if constexpr (LANES > 32) {
+    const auto b = __builtin_amdgcn_permlane32_swap(a_bits(v), a_bits(v), false, false);
+    v = a_float(b[0]) + a_float(b[1]);
+  }
+  return v;
 }
 // Sums of a and b over the block, in every thread; the order is fixed.
 __device__ __forceinline__ void block_sums(float &a, float &b, float *lds) {
-  a = wave_sum(a);
-  b = wave_sum(b);
+  a = lanes_sum(a);
+  b = lanes_sum(b);
   const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   __syncthreads();  // the last row's sums have been read
   if ((threadIdx.x & 63u) == 0) {
@@ -64,21 +70,23 @@ __device__ __forceinline__ void weight8(const void *w, uint32_t bf16, uint64_t c
 }
 
 // Rows of up to 16,384 entries stay in registers: GROUP threads have one, KEEP chunks of 8 each, and read it once.  A row goes to one
-// wave where that is enough (up to 2,048 entries) and there are rows for all, so that its sums need no barrier.
+// wave where that is enough (up to 2,048 entries) and there are rows for all, so that its sums need no barrier; a wave has two or
+// four of the short rows (up to 256 and 128 entries).
 //
 // A block's groups take a row each, the block then the next rows; all of them come round as often as each other.
 template <uint32_t GROUP, uint32_t KEEP>
 struct Fit {
   static constexpr uint32_t kGroup = GROUP, kKeep = KEEP;
   // whether the next row is loaded while one is worked on: where the registers last for it
-  static constexpr bool kAheadForward = GROUP < 1024, kAheadBackward = GROUP == 64 || (GROUP < 1024 && KEEP <= 3);
+  static constexpr bool kAheadForward = GROUP < 1024, kAheadBackward = GROUP <= 64 || (GROUP < 1024 && KEEP <= 3);
   static constexpr uint32_t kBlock = GROUP < 512 ? 512 : GROUP, kGroups = kBlock / GROUP;  // of the backward pass
 };
 // Sums of a and b over a group, in all its threads; the order is fixed.  All threads of the block come here.
 template <uint32_t GROUP>
 __device__ __forceinline__ void group_sums(float &a, float &b, af32x2 *lds) {
-  a = wave_sum(a);
-  b = wave_sum(b);
+  constexpr uint32_t kLanes = GROUP < 64 ? GROUP : 64;
+  a = lanes_sum<kLanes>(a);
+  b = lanes_sum<kLanes>(b);
   if constexpr (GROUP > 64) {
     const uint32_t wave = threadIdx.x >> 6, first = wave / (GROUP / 64) * (GROUP / 64);
     __syncthreads();  // the last sums have been read
@@ -103,26 +111,26 @@ struct Weight {
   const void *w;
   uint32_t bf16, cols, lds;
   float otherwise;
-  static constexpr uint32_t kLds = F::kGroup == 64 ? F::kKeep * 64 * 8 : 4;  // floats
+  static constexpr uint32_t kChunks = F::kGroup * F::kKeep, kLds = F::kGroup <= 64 ? kChunks * 8 : 4;  // floats
   __device__ __forceinline__ Weight(const void *w_, uint32_t bf16_, uint32_t cols_, float otherwise_, float *buffer)
       : w(w_), bf16(bf16_), cols(cols_), lds((uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)buffer), otherwise(otherwise_) {
     if constexpr (kHeld) {
 #pragma unroll
       for (uint32_t k = 0; k < F::kKeep; ++k) weight8(w, bf16, (threadIdx.x % F::kGroup + k * F::kGroup) * 8, cols, otherwise, v[k]);
-    } else if constexpr (F::kGroup == 64) {  // the chunks' first halves, then their second ones: 16 bytes a lane, side by side
-      for (uint32_t c = threadIdx.x; c < F::kKeep * 64; c += blockDim.x) {
+    } else if constexpr (F::kGroup <= 64) {  // the chunks' first halves, then their second ones: 16 bytes a lane, side by side
+      for (uint32_t c = threadIdx.x; c < kChunks; c += blockDim.x) {
         float u[8];
         weight8(w, bf16, c * 8, cols, otherwise, u);
         put(c, u[0], u[1], u[2], u[3]);
-        put(F::kKeep * 64 + c, u[4], u[5], u[6], u[7]);
+        put(kChunks + c, u[4], u[5], u[6], u[7]);
       }
     }
   }
   typedef __attribute__((address_space(3))) af32x4 lds_quad;
   __device__ __forceinline__ void put(uint32_t i, float a, float b, float c, float d) const { *reinterpret_cast<lds_quad *>(lds + i * 16) = af32x4{a, b, c, d}; }
   __device__ __forceinline__ void get(uint32_t k, uint32_t chunk, float (&u)[8]) const {
-    if constexpr (F::kGroup == 64) {
-      const af32x4 a = *reinterpret_cast<const lds_quad *>(lds + chunk * 16), b = *reinterpret_cast<const lds_quad *>(lds + (F::kKeep * 64 + chunk) * 16);
+    if constexpr (F::kGroup <= 64) {
+      const af32x4 a = *reinterpret_cast<const lds_quad *>(lds + chunk * 16), b = *reinterpret_cast<const lds_quad *>(lds + (kChunks + chunk) * 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) { u[i] = a[i]; u[4 + i] = b[i]; }
     } else if constexpr (kHeld) {
@@ -143,7 +151,7 @@ __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(Norm
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, cols = (uint32_t)in.cols;
   const float inv = 1.0f / (float)in.cols;
   const Weight<F> w(in.weight, in.bf16, cols, 1.0f, weights[0]), b(in.bias, in.bf16, cols, 0.0f, weights[1]);
-  if constexpr (F::kGroup == 64) __syncthreads();
+  if constexpr (F::kGroup <= 64) __syncthreads();
   Raw8<T> next[F::kKeep];
   auto load = [&](uint64_t r) {
     const uint8_t *x = static_cast<const uint8_t *>(in.x.data) + r * in.x.ld * kEntry<T>;
@@ -275,7 +283,7 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, group = threadIdx.x / F::kGroup, cols = (uint32_t)in.cols;
   const float inv = 1.0f / (float)in.cols;
   const Weight<F> w(in.weight, in.bf16, cols, 1.0f, weights);
-  if constexpr (F::kGroup == 64) __syncthreads();
+  if constexpr (F::kGroup <= 64) __syncthreads();
   float dw[F::kKeep][8], db[F::kKeep][8];
 #pragma unroll
   for (uint32_t k = 0; k < F::kKeep; ++k)
@@ -481,7 +489,7 @@ struct Kept {
 Kept kept(uint64_t rows, uint64_t cols) {
   const uint64_t chunks = ckpt_pitch(cols) / 8;
   // a wave to a row, unless there are fewer rows than make two waves for every SIMD: then four
-  uint32_t group = chunks <= 64 ? 64 : chunks <= 256 ? (rows < 2048 ? 256 : 64) : chunks <= 384 && rows >= 2048 ? 128 : chunks <= 1024 ? 256 : 1024;
+  uint32_t group = chunks <= 16 ? 16 : chunks <= 32 ? 32 : chunks <= 64 ? 64 : chunks <= 256 ? (rows < 2048 ? 256 : 64) : chunks <= 384 && rows >= 2048 ? 128 : chunks <= 1024 ? 256 : 1024;
   uint32_t keep = group == 128 ? 3 : 1;
   while (keep < (group == 1024 ? 2 : 4) && (uint64_t)group * keep < chunks) keep += group == 64 && keep == 2 ? 2 : 1;
   if ((uint64_t)group * keep < chunks) group = 0;
@@ -496,7 +504,7 @@ uint32_t norm_parts(uint64_t rows, uint64_t cols) {
 template <typename T, typename F>
 hipError_t run_norm(const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
   constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
-  const uint64_t blocks = (in.rows + kGroups - 1) / kGroups, most = 256 * (kBlock > 256 ? 1 : F::kGroup == 256 && F::kKeep > 2 ? 6 - F::kKeep : 4);
+  const uint64_t blocks = (in.rows + kGroups - 1) / kGroups, most = 256 * (kBlock > 256 ? 1 : F::kGroup == 256 && F::kKeep > 2 ? 6 - F::kKeep : F::kGroup == 128 ? 3 : 4);
   hipLaunchKernelGGL((k_norm<T, F>), dim3((uint32_t)(blocks < most ? blocks : most)), dim3(kBlock), 0, s, in, y, saved, mean, rstd);
   return hipGetLastError();
 }
@@ -507,6 +515,8 @@ hipError_t run_norm_grad(const NormGrad &in, float *part, uint32_t parts, hipStr
 }
 #define DQ_FITS(run, ...)                                       \
   switch (k.group * 8 + k.keep) {                               \
+    case 16 * 8 + 1: return run<T, Fit<16, 1>>(__VA_ARGS__);    \
+    case 32 * 8 + 1: return run<T, Fit<32, 1>>(__VA_ARGS__);    \
     case 64 * 8 + 1: return run<T, Fit<64, 1>>(__VA_ARGS__);    \
     case 64 * 8 + 2: return run<T, Fit<64, 2>>(__VA_ARGS__);    \
     case 64 * 8 + 4: return run<T, Fit<64, 4>>(__VA_ARGS__);    \

@@ -469,3 +469,25 @@ def test_gradients_against_differences(dev):
         e[k] = s
         want.view(-1)[k] = ((x.double() @ (2 * e.view_as(w)).t()) * d5.double()).sum() / (2 * s)
     assert float((dwl.double() - want).abs().max()) < 2e-5 * float(want.abs().max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 100), (33, 128), (5000, 129), (70, 256), (9, 200), (40000, 17), (20001, 250), (9000, 500), (2500, 3000), (600, 4099), (2200, 5000)])
+def test_layer_norm_of_every_way_to_keep_rows(dev, rows, cols, dtype):
+    """Short rows that share a wave, and blocks that take several rows."""
+    t = TYPES[dtype]
+    x, dy = acts(dev, rows, cols, t, rows + cols) + 0.5, acts(dev, rows, cols, t, rows + cols + 1)
+    weight, bias = (acts(dev, 1, cols, t, 3) * 0.2 + 1).reshape(-1), acts(dev, 1, cols, t, 4).reshape(-1)
+    y, saved = B.dq_layer_norm(x, weight, bias, save=True)
+    bound, dk, dm = P.layer_norm_bound(x, weight, bias, 1e-5, t)
+    want, mean, rstd = P.layer_norm(x, weight, bias, 1e-5)
+    within(y, want, bound, "y")
+    within(saved.mean, mean.reshape(-1), dm.reshape(-1), "mean")
+    within(saved.rstd, rstd.reshape(-1), (rstd * dk).reshape(-1), "rstd")
+    assert torch.equal(saved.x.data, B.dq_ckpt_save(x).data)
+    xv = P.held(x)
+    got = B.dq_layer_norm_grad(dy, saved, weight)
+    wants = P.layer_norm_grad(dy, xv, saved.mean, saved.rstd, weight)
+    bounds = P.layer_norm_grad_bounds(dy, xv, saved.mean, saved.rstd, weight, t, t)
+    for g, v, tol, what in zip(got, wants, bounds, ("dx", "dweight", "dbias")):
+        within(g, v, tol, what)
