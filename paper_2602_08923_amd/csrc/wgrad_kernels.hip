@@ -503,12 +503,12 @@ constexpr uint32_t kEdges[3] = {64, 128, 256}, kToks[2][3] = {{32, 32, 32}, {64,
 constexpr uint32_t kManySplits = 16;                                                       // of which several threads join one sum
 
 // The cut that costs least, by what was measured (MI355X, microseconds): a step of a block alone on its CU and of one among as many as
-// fit, the launch, and what splits add, a launch and their sums' way to memory and back at 5 TB/s.  Large tiles read and move
+// fit, the launch, the tiles' way to memory, and what splits add, a launch and their sums' way to memory and back at 5 TB/s.  Large tiles read and move
 // least for what they multiply; small ones and splits give every CU a part where sums are few.
 Cut cut_of(dq_dtype dtype, uint64_t rows, uint64_t outs, uint64_t cols) {
   constexpr uint64_t kCus = 256;
-  struct Cost { uint32_t fit; double alone, among; };  // blocks on a CU, a step's time
-  static constexpr Cost kCosts[2][3] = {{{3, 0.35, 0.78}, {2, 0.76, 1.39}, {1, 2.3, 2.3}}, {{3, 0.36, 0.79}, {2, 0.70, 1.12}, {1, 1.75, 1.75}}};
+  struct Cost { uint32_t fit; double alone, among, tile; };  // blocks on a CU, a step's time, their tiles' way to memory
+  static constexpr Cost kCosts[2][3] = {{{3, 0.33, 0.77, 4.2}, {2, 0.74, 1.37, 9.6}, {1, 2.25, 2.25, 21}}, {{3, 0.33, 0.78, 2.2}, {2, 0.65, 1.11, 4.1}, {1, 1.72, 1.72, 10}}};
   Cut best = {};
   double least = 0;
   for (uint32_t size = 0; size < (outs < 8 ? 1u : 3u); ++size) {
@@ -528,6 +528,7 @@ Cut cut_of(dq_dtype dtype, uint64_t rows, uint64_t outs, uint64_t cols) {
       double us = 3 + (double)each * ((double)(on_cu / cost.fit) * cost.among +
                                       (rest ? cost.alone + (cost.among - cost.alone) * (double)(rest - 1) / (cost.fit > 1 ? cost.fit - 1 : 1) : 0.0));
       if (splits > 1) us += 3 + (double)(splits * tiles * e * e) * 8 / 5.0e6;
+      else us += cost.tile * (double)on_cu / cost.fit;
       if ((size == 0 && k == 0) || us < least) {
         least = us;
         best = c;
