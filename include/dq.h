@@ -3,20 +3,22 @@
  * all-reduce (arxiv 2602.08923): first-hop compress, the fused
  * decompress-accumulate-recompress (DAR) hop, decompress(+accumulate), a driver that
  * replays ring / butterfly reduce-scatter hops for N simulated workers inside one
- * GPU's HBM, the same three calls for the OCP-MX comparison codec, and the steps on either
- * side of the main stage (statistics, bit allocation, reorder, restore).
+ * GPU's HBM, the same three calls for the OCP-MX comparison codec, the steps on either
+ * side of the main stage (statistics, bit allocation, reorder, restore), and the passes of a
+ * training step that its gradients come from, on activations kept in 8 bits.
  *
  * Conventions shared by every call
  *   - All data pointers are DEVICE pointers owned by the caller, 16-byte aligned
- *     (per-super-group arrays -- means, indices, statistics, positions -- 4-byte aligned;
+ *     (per-super-group arrays -- means, indices, statistics, positions -- 4-byte aligned, matrices
+ *     of activations and what belongs to their rows and columns aligned to their entries;
  *     DQ_EALIGN otherwise).  Descriptor structs (dq_config, dq_chunk, dq_local, dq_replay_desc
  *     and the arrays they point to) are HOST memory, read during the call only.
  *   - `hip_stream` is a hipStream_t (NULL = the default stream).  Calls enqueue work
  *     and return without synchronising; the library allocates device memory only in
  *     dq_create / dq_replay_create and never per call.
- *   - Errors are return codes only; on any error nothing has been enqueued.  Inputs
+ *   - Errors are return codes only; on any error nothing has been enqueued.  Gradients
  *     must be finite and partial sums must stay below the largest bf16: the library does
- *     not check this, and the result for other inputs is unspecified.  (Addresses in device
+ *     not check this, and the result for other inputs is unspecified (activations: see there).  (Addresses in device
  *     memory are computed from the descriptors alone, never from data values; the lookups
  *     in the on-chip tables are indexed by the normalised values and rely on finite inputs.)
  *   - The result of a call is a pure function of (config, chunk descriptor, rank,
@@ -154,8 +156,9 @@ dq_status dq_mx_decompress(dq_codec fmt, const void *packed_in, const void *loca
  * The calls below take matrices: row r of `rows` at data + r * ld entries (ld >= cols where there are several rows; a part of a
  * wider matrix is one), aligned to their entries, no more.  All matrices of a call have one type, except dw and what a load writes.
  * What a call writes must not overlap anything else it is given (DQ_EINVAL); two matrices side by side in a wider one do not
- * overlap.  rows or cols of zero: nothing is done, sums over no rows are zero.  Sums and statistics are binary32, in an order that
- * the sizes and types fix: the same call gives the same bits.  Infinities and NaN go where the formulas take them. */
+ * overlap (in one another's range, matrices of different ld count as overlapping).  rows or cols of zero: nothing is done, sums over
+ * no rows are zero.  Sums and statistics are binary32, in an order that the sizes and types fix: the same call gives the same bits.
+ * Infinities and NaN go where the formulas take them, with one exception (dq_ckpt_weight_grad). */
 typedef struct {
   void *data; /* device; read-only operands are not written */
   dq_dtype dtype;
@@ -172,7 +175,7 @@ dq_status dq_ckpt_load(const void *ckpt, uint64_t rows, uint64_t cols, const dq_
  *   dw[o][i] = sum over rows dy[.][o] x[.][i] (outs x cols),   db_or_null[o] = sum over rows dy[.][o] (of dw's type),
  * added to what is there if `accumulate`: in binary32, then rounded once to dw's type.  scratch: device memory of
  * dq_ckpt_weight_grad_scratch_bytes (of dy's type; may be 0, then NULL will do), 16-byte aligned, free again when the call's work
- * is done.  rows, outs and cols below 2^31. */
+ * is done.  rows, outs and cols below 2^31.  In a binary32 dy an infinity counts as NaN, and digits below 2^-133 are left out. */
 size_t dq_ckpt_weight_grad_scratch_bytes(dq_dtype dtype, uint64_t rows, uint64_t outs, uint64_t cols);
 dq_status dq_ckpt_weight_grad(const dq_matrix *dy, const void *ckpt, uint64_t rows, uint64_t outs, uint64_t cols, const dq_matrix *dw,
                               void *db_or_null, int accumulate, void *scratch, size_t scratch_bytes, void *hip_stream);
