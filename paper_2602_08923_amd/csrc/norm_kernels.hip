@@ -69,17 +69,19 @@ __device__ __forceinline__ void weight8(const void *w, uint32_t bf16, uint64_t c
   }
 }
 
-// Rows of up to 16,384 entries stay in registers: GROUP threads have one, KEEP chunks of 8 each, and read it once.  A row goes to one
-// wave where that is enough (up to 2,048 entries) and there are rows for all, so that its sums need no barrier; a wave has two or
-// four of the short rows (up to 256 and 128 entries).
+// Memory bounds both passes: rows of up to 16,384 entries stay in registers, so that they are read once.  GROUP threads have a row,
+// KEEP chunks of 8 entries each.  A row goes to one wave where that is enough (up to 2,048 entries) and there are rows for all, so that
+// its sums need no barrier; a wave has two or four of the short rows (up to 256 and 128 entries).  The next row is loaded while one
+// is worked on, and there are as many blocks as stay resident, so that most rows are loaded so.
+// Measured (forward and backward, 5.2 TB/s being a large copy's rate): bf16 16384 x 2048 72 us (4.7 TB/s), 200000 x 128 59 us (4.3),
+// 16384 x 4096 135 us (5.0), 4096 x 16384 169 us (4.0); fp32 1021 x 6151 38 us (3.0).
 //
 // A block's groups take a row each, the block then the next rows; all of them come round as often as each other.
 template <uint32_t GROUP, uint32_t KEEP>
 struct Fit {
   static constexpr uint32_t kGroup = GROUP, kKeep = KEEP;
-  // whether the next row is loaded while one is worked on: where the registers last for it
-  static constexpr bool kAheadForward = GROUP < 1024, kAheadBackward = GROUP <= 64 || (GROUP < 1024 && KEEP <= 3);
-  static constexpr uint32_t kBlock = GROUP < 512 ? 512 : GROUP, kGroups = kBlock / GROUP;  // of the backward pass
+  static constexpr bool kAheadBackward = GROUP <= 64 || KEEP <= 3;  // with more, the backward pass has no registers to load ahead
+  static constexpr uint32_t kBlock = 512, kGroups = kBlock / GROUP;  // of the backward pass
 };
 // Sums of a and b over a group, in all its threads; the order is fixed.  All threads of the block come here.
 template <uint32_t GROUP>
@@ -102,22 +104,20 @@ __device__ __forceinline__ void group_sums(float &a, float &b, af32x2 *lds) {
   }
 }
 
-// A weight (or a bias) as the threads of a group read it, eight entries at a time: where a wave has a row, from LDS, which leaves it
-// registers for the next row; else from registers, of which 1,024 threads have too few: they read it from memory each time.
+// A weight (or a bias) as the threads of a group read it, eight entries at a time: from registers, or, where a wave has a row and many
+// rows pass, from LDS, which leaves registers for the next row.
 template <typename F>
 struct Weight {
-  static constexpr bool kHeld = F::kGroup == 128 || F::kGroup == 256;
-  float v[kHeld ? F::kKeep : 1][8];
-  const void *w;
-  uint32_t bf16, cols, lds;
-  float otherwise;
-  static constexpr uint32_t kChunks = F::kGroup * F::kKeep, kLds = F::kGroup <= 64 ? kChunks * 8 : 4;  // floats
-  __device__ __forceinline__ Weight(const void *w_, uint32_t bf16_, uint32_t cols_, float otherwise_, float *buffer)
-      : w(w_), bf16(bf16_), cols(cols_), lds((uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)buffer), otherwise(otherwise_) {
-    if constexpr (kHeld) {
+  static constexpr bool kInLds = F::kGroup <= 64;
+  static constexpr uint32_t kChunks = F::kGroup * F::kKeep, kLds = kInLds ? kChunks * 8 : 4;  // floats
+  float v[kInLds ? 1 : F::kKeep][8];
+  uint32_t lds;
+  __device__ __forceinline__ Weight(const void *w, uint32_t bf16, uint32_t cols, float otherwise, float *buffer)
+      : lds((uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)buffer) {
+    if constexpr (!kInLds) {
 #pragma unroll
       for (uint32_t k = 0; k < F::kKeep; ++k) weight8(w, bf16, (threadIdx.x % F::kGroup + k * F::kGroup) * 8, cols, otherwise, v[k]);
-    } else if constexpr (F::kGroup <= 64) {  // the chunks' first halves, then their second ones: 16 bytes a lane, side by side
+    } else {  // the chunks' first halves, then their second ones: 16 bytes a lane, side by side
       for (uint32_t c = threadIdx.x; c < kChunks; c += blockDim.x) {
         float u[8];
         weight8(w, bf16, c * 8, cols, otherwise, u);
@@ -129,15 +129,13 @@ struct Weight {
   typedef __attribute__((address_space(3))) af32x4 lds_quad;
   __device__ __forceinline__ void put(uint32_t i, float a, float b, float c, float d) const { *reinterpret_cast<lds_quad *>(lds + i * 16) = af32x4{a, b, c, d}; }
   __device__ __forceinline__ void get(uint32_t k, uint32_t chunk, float (&u)[8]) const {
-    if constexpr (F::kGroup <= 64) {
+    if constexpr (kInLds) {
       const af32x4 a = *reinterpret_cast<const lds_quad *>(lds + chunk * 16), b = *reinterpret_cast<const lds_quad *>(lds + (kChunks + chunk) * 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) { u[i] = a[i]; u[4 + i] = b[i]; }
-    } else if constexpr (kHeld) {
+    } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) u[i] = v[k][i];
-    } else {
-      weight8(w, bf16, chunk * 8, cols, otherwise, u);
     }
   }
 };
@@ -145,13 +143,12 @@ struct Weight {
 template <typename T, typename F>
 __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(NormIn in, Rows y, CkptOut saved, float *mean, float *rstd) {
   constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
-  constexpr bool kAhead = F::kAheadForward;
   __shared__ af32x2 lds[kBlock / 64];
   __shared__ __attribute__((aligned(16))) float weights[2][Weight<F>::kLds];
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, cols = (uint32_t)in.cols;
   const float inv = 1.0f / (float)in.cols;
   const Weight<F> w(in.weight, in.bf16, cols, 1.0f, weights[0]), b(in.bias, in.bf16, cols, 0.0f, weights[1]);
-  if constexpr (F::kGroup <= 64) __syncthreads();
+  if constexpr (Weight<F>::kInLds) __syncthreads();
   Raw8<T> next[F::kKeep];
   auto load = [&](uint64_t r) {
     const uint8_t *x = static_cast<const uint8_t *>(in.x.data) + r * in.x.ld * kEntry<T>;
@@ -164,14 +161,13 @@ __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(Norm
   };
   const uint64_t step = (uint64_t)gridDim.x * kGroups;
   uint64_t r = (uint64_t)blockIdx.x * kGroups + threadIdx.x / F::kGroup;
-  if (kAhead) load(r);
+  load(r);
   for (uint64_t first = (uint64_t)blockIdx.x * kGroups; first < in.rows; first += step, r += step) {
     const bool here = r < in.rows;
-    if (!kAhead) load(r);
     float v[F::kKeep][8], s = 0.0f, none = 0.0f;
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) widen8<T>(next[k], v[k]);
-    if (kAhead) load(r + step);
+    load(r + step);
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k)
 #pragma unroll
@@ -283,7 +279,7 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, group = threadIdx.x / F::kGroup, cols = (uint32_t)in.cols;
   const float inv = 1.0f / (float)in.cols;
   const Weight<F> w(in.weight, in.bf16, cols, 1.0f, weights);
-  if constexpr (F::kGroup <= 64) __syncthreads();
+  if constexpr (Weight<F>::kInLds) __syncthreads();
   float dw[F::kKeep][8], db[F::kKeep][8];
 #pragma unroll
   for (uint32_t k = 0; k < F::kKeep; ++k)
@@ -482,16 +478,18 @@ __global__ __launch_bounds__(kJoinThreads) void k_norm_join(const float *part, u
 constexpr uint32_t kRowBlocks = 512;  // blocks that longer rows are dealt to
 uint32_t row_blocks(uint64_t rows) { return (uint32_t)(rows < kRowBlocks ? rows : kRowBlocks); }
 
-// How rows are kept: threads to a row and chunks to a thread (group 0: the row is too long).
+// How rows are kept: threads to a row and chunks to a thread (group 0: the row is too long).  Measured, forward and backward:
+// 16384 x 2056 in bf16 takes 89 us by groups of 128, 116 by 256; 4096 x 16384 169 us by groups of 512 that load ahead, 185 by 1,024 that
+// have no registers for it.
 struct Kept {
   uint32_t group, keep;
 };
 Kept kept(uint64_t rows, uint64_t cols) {
   const uint64_t chunks = ckpt_pitch(cols) / 8;
   // a wave to a row, unless there are fewer rows than make two waves for every SIMD: then four
-  uint32_t group = chunks <= 16 ? 16 : chunks <= 32 ? 32 : chunks <= 64 ? 64 : chunks <= 256 ? (rows < 2048 ? 256 : 64) : chunks <= 384 && rows >= 2048 ? 128 : chunks <= 1024 ? 256 : 1024;
+  uint32_t group = chunks <= 16 ? 16 : chunks <= 32 ? 32 : chunks <= 64 ? 64 : chunks <= 256 ? (rows < 2048 ? 256 : 64) : chunks <= 384 && rows >= 2048 ? 128 : chunks <= 1024 ? 256 : 512;
   uint32_t keep = group == 128 ? 3 : 1;
-  while (keep < (group == 1024 ? 2 : 4) && (uint64_t)group * keep < chunks) keep += group == 64 && keep == 2 ? 2 : 1;
+  while (keep < 4 && (uint64_t)group * keep < chunks) keep += group == 64 && keep == 2 ? 2 : 1;
   if ((uint64_t)group * keep < chunks) group = 0;
   return {group, keep};
 }
@@ -525,7 +523,8 @@ hipError_t run_norm_grad(const NormGrad &in, float *part, uint32_t parts, hipStr
     case 256 * 8 + 2: return run<T, Fit<256, 2>>(__VA_ARGS__);  \
     case 256 * 8 + 3: return run<T, Fit<256, 3>>(__VA_ARGS__);  \
     case 256 * 8 + 4: return run<T, Fit<256, 4>>(__VA_ARGS__);  \
-    case 1024 * 8 + 2: return run<T, Fit<1024, 2>>(__VA_ARGS__); \
+    case 512 * 8 + 3: return run<T, Fit<512, 3>>(__VA_ARGS__);  \
+    case 512 * 8 + 4: return run<T, Fit<512, 4>>(__VA_ARGS__);  \
   }
 template <typename T>
 hipError_t norm_forward(const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
