@@ -491,3 +491,121 @@ def test_layer_norm_of_every_way_to_keep_rows(dev, rows, cols, dtype):
     bounds = P.layer_norm_grad_bounds(dy, xv, saved.mean, saved.rstd, weight, t, t)
     for g, v, tol, what in zip(got, wants, bounds, ("dx", "dweight", "dbias")):
         within(g, v, tol, what)
+
+
+def test_captured_gradients_add_up(dev):
+    """Gradients added to a bucket inside a graph: each replay adds once more, split sums and joined parts among them; whole numbers, exact."""
+    rows, outs, cols = 5000, 70, 90
+    g = gen(dev, 1)
+    x = torch.randint(-7, 8, (rows, cols), generator=g, device=dev).to(torch.bfloat16)
+    dy = torch.randint(-9, 10, (rows, outs), generator=g, device=dev).to(torch.bfloat16)
+    assert B.lib().dq_ckpt_weight_grad_scratch_bytes(B.DQ_BF16, rows, outs, cols) > 0
+    want, want_b = P.weight_grad(dy, P.held(x))
+    dw, db = torch.zeros(outs, cols, device=dev), torch.zeros(outs, device=dev)
+    weight = torch.ones(cols, device=dev)
+    bias_sum = torch.zeros(cols, device=dev)
+    weight_sum = torch.zeros(cols, device=dev)
+
+    def step():
+        ck = B.dq_ckpt_save(x)
+        B.dq_ckpt_weight_grad(dy, ck, out=dw, bias_out=db, accumulate=True)
+        _, saved = B.dq_layer_norm(x, weight, save=True)
+        B.dq_layer_norm_grad(x, saved, weight, weight_out=weight_sum, bias_out=bias_sum, accumulate=True)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    times = 1
+    for _ in range(4):
+        graph.replay()
+        other = B.dq_ckpt_weight_grad(dy.flip(0).contiguous(), B.dq_ckpt_save(x), bias=True)     # the program's own work between replays
+        torch.cuda.synchronize()
+        times += 1
+        assert torch.equal(dw.double(), times * want) and torch.equal(db.double(), times * want_b), times
+        assert torch.equal(bias_sum.double(), times * x.double().sum(0)), times
+        assert torch.equal(other[1].double(), want_b.to(torch.bfloat16).double())
+
+
+def test_two_graphs_of_one_pool_and_two_streams_at_once(dev):
+    x, dy = [acts(dev, 3000, 200, torch.bfloat16, s) for s in (1, 2)], [acts(dev, 3000, 100, torch.bfloat16, s) for s in (3, 4)]
+
+    def work(k):
+        y, saved = B.dq_layer_norm(x[k], save=True)
+        return B.dq_ckpt_weight_grad(dy[k], B.dq_ckpt_save(y), bias=True) + (B.dq_layer_norm_grad(x[k], saved, torch.ones(200, device=dev))[1],)
+
+    want = [[t.clone() for t in work(k)] for k in (0, 1)]
+    torch.cuda.synchronize()
+    graphs, got, pool = [], [], torch.cuda.graph_pool_handle()
+    for k in (0, 1):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[k], pool=pool):
+            got.append(work(k))
+    for k in (0, 1, 1, 0, 1):                       # one after the other, as graphs that share a pool are replayed
+        graphs[k].replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got[k], want[k]):
+            assert torch.equal(a, b)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        outs = []
+        for k, s in enumerate(streams):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                outs.append(work(k))
+        torch.cuda.synchronize()
+        for k in (0, 1):
+            for a, b in zip(outs[k], want[k]):
+                assert torch.equal(a, b)
+
+
+def test_out_arguments_and_refusals_of_shapes(dev):
+    x = acts(dev, 6, 64, torch.bfloat16, 1)
+    ck = B.dq_ckpt_save(x)
+    out = torch.zeros(B.dq_ckpt_bytes(6, 64) + 32, dtype=torch.uint8, device=dev)
+    again = B.dq_ckpt_save(x, out)
+    assert again.data is out and torch.equal(out[:ck.data.numel()], ck.data) and not out[ck.data.numel():].any()
+    _, saved = B.dq_layer_norm(x, save=True)
+    h, gate = B.dq_gate(x, x.flip(0).contiguous(), save=True)
+    w = torch.ones(64, device=dev)
+    for call, match in [
+        (lambda: B.dq_ckpt_save(x.t()), "side by side"),
+        (lambda: B.dq_ckpt_save(x[:1].expand(6, 64)), "not overlap"),
+        (lambda: B.dq_ckpt_save(x.reshape(2, 3, 64)[:, :2]), "one distance"),
+        (lambda: B.dq_ckpt_save(x.half()), "float32 or bfloat16"),
+        (lambda: B.dq_ckpt_save(x, out[:100]), "all its bytes"),
+        (lambda: B.dq_ckpt_save(x, out[8:]), "aligned"),
+        (lambda: B.dq_ckpt_save(x[0, 0]), "dimension"),
+        (lambda: B.dq_ckpt_load(ck, torch.float16), "float32 or bfloat16"),
+        (lambda: B.dq_ckpt_load(ck, out=torch.empty(6, 63, device=dev)), "another shape"),
+        (lambda: B.dq_ckpt_load(B.Checkpoint(ck.data, 7, 64)), "all its bytes"),
+        (lambda: B.dq_ckpt_load(B.Checkpoint(ck.data, -1, 64)), "not negative"),
+        (lambda: B.dq_ckpt_weight_grad(x[:5], ck), "rows"),
+        (lambda: B.dq_ckpt_weight_grad(x, ck, out=torch.empty(64, 63, device=dev)), "another shape"),
+        (lambda: B.dq_ckpt_weight_grad(x, ck, accumulate=True), "give them"),
+        (lambda: B.dq_ckpt_weight_grad(x, ck, out=torch.empty(64, 64, device=dev), bias=True, accumulate=True), "give them"),
+        (lambda: B.dq_ckpt_weight_grad(x, ck, bias_out=torch.empty(63, dtype=x.dtype, device=dev)), "bias_out"),
+        (lambda: B.dq_layer_norm(x, torch.ones(63, device=dev)), "weight"),
+        (lambda: B.dq_layer_norm(x, w, w.bfloat16()), "bias"),
+        (lambda: B.dq_layer_norm(x, eps=-1.0), "invalid"),
+        (lambda: B.dq_layer_norm(x, out=x), "invalid"),
+        (lambda: B.dq_layer_norm(x, out=torch.empty(6, 64, device=dev)), "another type"),
+        (lambda: B.dq_layer_norm_grad(x[:5], saved, w), "another shape"),
+        (lambda: B.dq_layer_norm_grad(x, saved, w, accumulate=True), "give them"),
+        (lambda: B.dq_layer_norm_grad(x, saved, None, weight_out=w), "without a weight"),
+        (lambda: B.dq_layer_norm_grad(x, saved, w, weight_out=w), "invalid"),
+        (lambda: B.dq_gate(x, x[:, :32]), "another shape"),
+        (lambda: B.dq_gate(x, x.float()), "another type"),
+        (lambda: B.dq_gate_grad(x[:5], gate), "another shape"),
+        (lambda: B.dq_gate_grad(x, gate._replace(u=None), u_out=torch.empty_like(x)), "no u"),
+        (lambda: B.dq_gate_grad(x, gate, z_out=h, u_out=h), "invalid"),
+        (lambda: B.dq_gate_grad(x, gate, z_out=x), "invalid"),
+        (lambda: B.dq_layer_norm(x, w.cpu()), "different devices"),
+    ]:
+        with pytest.raises(B.DqError, match=match):
+            call()
+    torch.cuda.synchronize()
