@@ -480,14 +480,16 @@ uint32_t row_blocks(uint64_t rows) { return (uint32_t)(rows < kRowBlocks ? rows 
 
 // How rows are kept: threads to a row and chunks to a thread (group 0: the row is too long).  Measured, forward and backward:
 // 16384 x 2056 in bf16 takes 89 us by groups of 128, 116 by 256; 4096 x 16384 169 us by groups of 512 that load ahead, 185 by 1,024 that
-// have no registers for it.
+// have no registers for it; 200000 x 128 59 us by groups of 16, 150 by 64.  Few rows are shared by more threads: the two kernels take 6
+// and 11 us for 1024 x 2048 by groups of 64, 6 and 7 by 256 (256 rows: 5 and 10, 4 and 4; 3000: 10 and 15, 11 and 12; 6000: 14 and 18, 17
+// and 19), for 2000 x 1024 5 and 7 by 64, 7 and 8 by 256.
 struct Kept {
   uint32_t group, keep;
 };
 Kept kept(uint64_t rows, uint64_t cols) {
   const uint64_t chunks = ckpt_pitch(cols) / 8;
-  // a wave to a row, unless there are fewer rows than make two waves for every SIMD: then four
-  uint32_t group = chunks <= 16 ? 16 : chunks <= 32 ? 32 : chunks <= 64 ? 64 : chunks <= 256 ? (rows < 2048 ? 256 : 64) : chunks <= 384 && rows >= 2048 ? 128 : chunks <= 1024 ? 256 : 512;
+  const uint64_t few = chunks <= 128 ? 1024 : 4096;
+  uint32_t group = chunks <= 16 ? 16 : chunks <= 32 ? 32 : chunks <= 64 ? 64 : chunks <= 256 ? (rows < few ? 256 : 64) : chunks <= 384 && rows >= 2048 ? 128 : chunks <= 1024 ? 256 : 512;
   uint32_t keep = group == 128 ? 3 : 1;
   while (keep < 4 && (uint64_t)group * keep < chunks) keep += group == 64 && keep == 2 ? 2 : 1;
   if ((uint64_t)group * keep < chunks) group = 0;

@@ -505,7 +505,7 @@ struct Cut {
   uint64_t tiles_out, tiles_in, split_rows;
 };
 constexpr uint32_t kEdges[3] = {64, 128, 256}, kToks[2][3] = {{32, 32, 32}, {64, 64, 64}};  // [bf16][size]
-constexpr uint32_t kManySplits = 16;                                                       // of which several threads join one sum
+constexpr uint32_t kManySplits = 16;  // of which several threads join one sum (30000 x 64 x 64, a hundred splits: 10 us; 40 by one thread a sum)
 
 // The cut that costs least, by what was measured (MI355X, microseconds): a step of a block alone on its CU and of one among as many as
 // fit, the launch, the tiles' way to memory, and what splits add, a launch and their sums' way to memory and back at 5 TB/s.  Large tiles read and move
