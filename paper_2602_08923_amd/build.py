@@ -50,7 +50,7 @@ def _extension_command():
             "-I", sysconfig.get_path("include"), "-isystem", os.path.join(t, "include"),
             "-isystem", os.path.join(t, "include", "torch", "csrc", "api", "include"), "-isystem", os.path.join(rocm, "include"),
             "-I", os.path.join(ROOT, "include"), "-I", CSRC, os.path.join(CSRC, "dq_python.cpp"), "-o", EXT,
-            "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+            "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip"]
 
 
 def build(verbose=False, extra_flags=()):

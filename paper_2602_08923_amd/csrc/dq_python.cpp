@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
@@ -616,9 +617,11 @@ void *vector_of(const at::Tensor *t, int64_t n, at::ScalarType type, const char 
   if (t->numel() != n || t->scalar_type() != type) fail(std::string(name) + " has another length or type");
   return ptr(*t);
 }
+// New memory, past the dispatcher (0.3 us a tensor less; these calls make up to five, and take 4 to 10 us).
 at::Tensor make_shaped(at::IntArrayRef shape, at::ScalarType t, const at::Tensor &like) {
-  return unlocked([&] { return at::empty(shape, like.options().dtype(t)); });
+  return unlocked([&] { return at::Tensor(at::detail::empty_cuda(shape, t, like.device(), c10::nullopt)); });
 }
+at::Tensor make_row(int64_t n, at::ScalarType t, const at::Tensor &like) { return make_shaped({n}, t, like); }
 // A checkpoint's tensor, rows and columns as three arguments.
 struct Saved {
   const at::Tensor *data = nullptr;
@@ -646,7 +649,7 @@ Saved saved_of(PyObject *const *a, const OnDevice &here) {
 at::Tensor ckpt_new(PyObject *given, const Act &x, const at::Tensor &like, const OnDevice &here) {
   const uint64_t bytes = L.dq_ckpt_bytes((uint64_t)x.rows, (uint64_t)x.cols);
   if (x.rows && x.cols && !bytes) fail("a checkpoint of so many rows and columns does not exist");
-  if (given == Py_None) return make((int64_t)bytes, at::kByte, like);
+  if (given == Py_None) return make_row((int64_t)bytes, at::kByte, like);
   const at::Tensor &t = tensor(given);
   here.with(t);
   ckpt_ptr(t, x.rows, x.cols);
@@ -706,13 +709,13 @@ PyObject *py_ckpt_weight_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, da
   if (w.rows != g.cols || w.cols != x.cols) fail("out has another shape");
   at::Tensor db;
   if (bias) {
-    db = a[6] == Py_None ? make(g.cols, out.scalar_type(), out) : tensor(a[6]);
+    db = a[6] == Py_None ? make_row(g.cols, out.scalar_type(), out) : tensor(a[6]);
     here.with(db);
   }
   void *d = bias ? vector_of(&db, g.cols, out.scalar_type(), "bias_out") : nullptr;
   at::Tensor scratch;  // free again when the call returns: what is enqueued on its stream next may have the memory
   const size_t bytes = L.dq_ckpt_weight_grad_scratch_bytes(g.m.dtype, g.rows, g.cols, x.cols);
-  if (bytes) scratch = make((int64_t)bytes, at::kByte, dy);
+  if (bytes) scratch = make_row((int64_t)bytes, at::kByte, dy);
   void *t = bytes ? scratch.data_ptr() : nullptr, *i = ckpt_ptr(*x.data, x.rows, x.cols), *s = stream();
   CALL(dq_ckpt_weight_grad(&g.m, i, g.rows, g.cols, x.cols, &w.m, d, accumulate, t, bytes, s));
   return bias ? pair(give(a[4], out), give(a[6], db)) : give(a[4], out);
@@ -743,8 +746,8 @@ PyObject *py_layer_norm(PyObject *const *a, Py_ssize_t nargs) {  // x, weight, b
   at::Tensor ckpt, mean, rstd;
   if (save) {
     ckpt = ckpt_new(Py_None, m, x, here);
-    mean = make(m.rows, at::kFloat, x);
-    rstd = make(m.rows, at::kFloat, x);
+    mean = make_row(m.rows, at::kFloat, x);
+    rstd = make_row(m.rows, at::kFloat, x);
   }
   void *c = save ? ckpt.data_ptr() : nullptr, *s = stream();
   float *mu = save ? as<float>(mean.data_ptr()) : nullptr, *rs = save ? as<float>(rstd.data_ptr()) : nullptr;
@@ -776,14 +779,14 @@ PyObject *py_layer_norm_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, dat
   void *pw = nullptr, *pb = nullptr, *t = nullptr;
   size_t bytes = 0;
   if (weight) {
-    dw = a[8] == Py_None ? make(g.cols, wt, dy) : tensor(a[8]);
-    db = a[9] == Py_None ? make(g.cols, wt, dy) : tensor(a[9]);
+    dw = a[8] == Py_None ? make_row(g.cols, wt, dy) : tensor(a[8]);
+    db = a[9] == Py_None ? make_row(g.cols, wt, dy) : tensor(a[9]);
     here.with(dw);
     here.with(db);
     pw = vector_of(&dw, g.cols, wt, "weight_out");
     pb = vector_of(&db, g.cols, wt, "bias_out");
     bytes = L.dq_layer_norm_grad_scratch_bytes(g.rows, g.cols);
-    if (bytes) scratch = make((int64_t)bytes, at::kByte, dy);  // free again when the call returns, as above
+    if (bytes) scratch = make_row((int64_t)bytes, at::kByte, dy);  // free again when the call returns, as above
     t = bytes ? scratch.data_ptr() : nullptr;
   }
   void *c = ckpt_ptr(*x.data, x.rows, x.cols), *s = stream();
