@@ -12,8 +12,9 @@ namespace {
 
 constexpr uint32_t kWideThreads = 1024, kThreads = 256;
 
-// The sum over a wave, or over each 16 or 32 of its lanes, in all of them: within rows of 16 lanes by moves that the addition makes itself, then over the rows (a swap
-// of two copies' rows, or halves, leaves what is to be added in the two).  Through LDS, as shuffles go, a sum took 100 cycles a step.
+// The sum over a wave, or over each 16 or 32 of its lanes, in all of them: within rows of 16 lanes by moves that the addition makes
+// itself, then over the rows (a swap of two copies' rows, or halves, leaves what is to be added in the two).  Through LDS, as
+// shuffles go, a sum took 100 cycles a step.
 template <int CTRL>
 __device__ __forceinline__ float add_dpp(float v) {
   return v + a_float((uint32_t)__builtin_amdgcn_mov_dpp((int)a_bits(v), CTRL, 0xF, 0xF, true));
@@ -269,13 +270,13 @@ struct NormGrad {
 };
 
 // The backward pass of rows that stay in registers, with the sums over rows beside: a thread's columns are the same in all of its
-// rows, so it sums them up as they pass; at the end the block's groups add up in turn and the block's sums go to `part`
+// rows, so it sums them up as they pass; at the end the block's groups add up and the block's sums go to `part`
 // ([blocks][2][pitch]).  One block of 512 threads to a CU (8 waves have what it takes in flight), so that there are few.
 template <typename T, typename F>
 __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *part) {
   constexpr bool kAhead = F::kAheadBackward;
   __shared__ af32x2 lds[F::kBlock / 64];
-  __shared__ __attribute__((aligned(16))) float weights[Weight<F>::kLds], sums[F::kGroups > 1 ? F::kGroup * F::kKeep * 16 : 4];
+  __shared__ __attribute__((aligned(16))) float weights[Weight<F>::kLds], sums[F::kGroups > 1 ? F::kGroups / 2 * F::kGroup * F::kKeep * 16 : 4];
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, group = threadIdx.x / F::kGroup, cols = (uint32_t)in.cols;
   const float inv = 1.0f / (float)in.cols;
   const Weight<F> w(in.weight, in.bf16, cols, 1.0f, weights);
@@ -353,34 +354,51 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
   }
   if (!part) return;
   float *out = part + (uint64_t)blockIdx.x * 2 * chunks * 8;
-  for (uint32_t turn = 0; turn < F::kGroups; ++turn) {
-    if (group == turn) {
+  // The upper half of the groups leaves its sums in LDS, the lower half adds them, until one group has them all.
+  typedef __attribute__((address_space(3))) af32x4 lds_quad;
+  constexpr uint32_t kSlot = F::kGroup * F::kKeep * 4;  // quads of a group's sums, in four parts: 16 bytes a lane, side by side
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)sums + me * 16;
 #pragma unroll
-      for (uint32_t k = 0; k < F::kKeep; ++k) {
-        const uint32_t c = me + k * F::kGroup;
-        if (c >= chunks) continue;
+  for (uint32_t half = F::kGroups / 2; half; half /= 2) {
+    const bool gives = group >= half && group < 2 * half, takes = group < half;
+    const uint32_t slot = base + (gives ? group - half : group) * (kSlot * 16);
+    if (gives) {
+#pragma unroll
+      for (uint32_t k = 0; k < F::kKeep; ++k)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          float *at = sums + (k * F::kGroup + me) * 4 + h * F::kGroup * F::kKeep * 4;  // (16 bytes a lane: no bank is asked twice)
-          af32x4 a = {dw[k][4 * h], dw[k][4 * h + 1], dw[k][4 * h + 2], dw[k][4 * h + 3]}, b = {db[k][4 * h], db[k][4 * h + 1], db[k][4 * h + 2], db[k][4 * h + 3]};
-          constexpr uint32_t kDb = F::kGroup * F::kKeep * 8;
-          if constexpr (F::kGroups > 1) {
-            if (turn) {
-              a += *reinterpret_cast<af32x4 *>(at);
-              b += *reinterpret_cast<af32x4 *>(at + kDb);
-            }
-            if (turn + 1 < F::kGroups) {
-              *reinterpret_cast<af32x4 *>(at) = a;
-              *reinterpret_cast<af32x4 *>(at + kDb) = b;
-              continue;
-            }
-          }
-          a_st<af32x4>(out + c * 8 + 4 * h, a);
-          a_st<af32x4>(out + chunks * 8 + c * 8 + 4 * h, b);
+          lds_quad *at = reinterpret_cast<lds_quad *>(slot + (h * F::kKeep + k) * (F::kGroup * 16));
+          *at = af32x4{dw[k][4 * h], dw[k][4 * h + 1], dw[k][4 * h + 2], dw[k][4 * h + 3]};
+          at[kSlot / 2] = af32x4{db[k][4 * h], db[k][4 * h + 1], db[k][4 * h + 2], db[k][4 * h + 3]};
         }
-      }
     }
-    if constexpr (F::kGroups > 1) __syncthreads();
+    __syncthreads();
+    if (takes) {
+#pragma unroll
+      for (uint32_t k = 0; k < F::kKeep; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const lds_quad *at = reinterpret_cast<const lds_quad *>(slot + (h * F::kKeep + k) * (F::kGroup * 16));
+          const af32x4 a = *at, b = at[kSlot / 2];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            dw[k][4 * h + i] += a[i];
+            db[k][4 * h + i] += b[i];
+          }
+        }
+    }
+    __syncthreads();
+  }
+  if (group) return;
+#pragma unroll
+  for (uint32_t k = 0; k < F::kKeep; ++k) {
+    const uint32_t c = me + k * F::kGroup;
+    if (c >= chunks) continue;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      a_st<af32x4>(out + c * 8 + 4 * h, af32x4{dw[k][4 * h], dw[k][4 * h + 1], dw[k][4 * h + 2], dw[k][4 * h + 3]});
+      a_st<af32x4>(out + chunks * 8 + c * 8 + 4 * h, af32x4{db[k][4 * h], db[k][4 * h + 1], db[k][4 * h + 2], db[k][4 * h + 3]});
+    }
   }
 }
 
