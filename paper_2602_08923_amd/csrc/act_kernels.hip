@@ -2,8 +2,8 @@
 // and whose backward pass reads them from there.
 //
 // All are streams: every entry is read once and written once, a few dozen operations each, so memory bounds them.  Measured: a
-// checkpoint of bf16 16384 x 8192, saved and loaded, 159 us (5.1 TB/s), SiLU with a gate there, forward and backward, 430 us (5.0), GELU
-// at 16384 x 4096 137 us (4.9; with a gate 215, 5.0); rows off 16-byte borders up to 15 % more.
+// checkpoint of bf16 16384 x 8192, saved and loaded, 134 us (6.1 TB/s), SiLU with a gate there, forward and backward, 351 us (6.1), GELU
+// at 16384 x 4096 125 us (5.4; with a gate 187, 5.8); rows off 16-byte borders up to 40 % more.
 #include <atomic>
 #include <initializer_list>
 
@@ -15,18 +15,27 @@ namespace {
 constexpr uint32_t kMapThreads = 256;
 
 // Here a lane's chunk is 16 bytes of a row, so that a wave's loads and stores each cover memory without gaps: 8 entries of bf16, 4 of
-// binary32 (with 8 of them, 32 bytes, half of each line a store touched came with the next one: 16384 x 4096, saved and loaded, took 174 us, not 146).
+// binary32 (with 8 of them, 32 bytes, half of each line a store touched came with the next one: 16384 x 4096, saved and loaded through the caches, took 174 us, not 146).
 template <typename T>
 constexpr uint32_t kChunk = 16 / kEntry<T>;
 template <typename T>
 struct Chunk {
   float v[kChunk<T>];
 };
-template <typename T>
+// PAST: past the caches, in large calls (see plan_map).
+template <typename T, bool PAST>
 __device__ __forceinline__ Chunk<T> load_chunk(const void *row, uint64_t at, uint64_t cols) {
   Chunk<T> c;
   const uint64_t col = at * kChunk<T>;
-  if constexpr (__is_same(T, F32)) {
+  if (PAST && col + kChunk<T> <= cols) {
+    const a32x4 q = __builtin_nontemporal_load(static_cast<const __attribute__((address_space(1))) a32x4 *>((const __attribute__((address_space(1))) void *)row) + at);
+    if constexpr (__is_same(T, F32)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c.v[i] = a_float(q[i]);
+    } else {
+      widen8<T>(Raw8<T>{{q}}, c.v);
+    }
+  } else if constexpr (__is_same(T, F32)) {
     const uint8_t *p = static_cast<const uint8_t *>(row) + col * 4;
     if (col + 4 <= cols) {
       const af32x4 q = a_ld<af32x4_any>(p);
@@ -41,10 +50,18 @@ __device__ __forceinline__ Chunk<T> load_chunk(const void *row, uint64_t at, uin
   }
   return c;
 }
-template <typename T>
+template <typename T, bool PAST>
 __device__ __forceinline__ void store_chunk(void *row, uint64_t at, uint64_t cols, const Chunk<T> &c) {
   const uint64_t col = at * kChunk<T>;
-  if constexpr (__is_same(T, F32)) {
+  if (PAST && col + kChunk<T> <= cols) {
+    a32x4 q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (__is_same(T, F32)) q[i] = a_bits(c.v[i]);
+      else q[i] = to_bf16x2(c.v[2 * i], c.v[2 * i + 1]);
+    }
+    __builtin_nontemporal_store(q, static_cast<__attribute__((address_space(1))) a32x4 *>((__attribute__((address_space(1))) void *)row) + at);
+  } else if constexpr (__is_same(T, F32)) {
     uint8_t *p = static_cast<uint8_t *>(row) + col * 4;
     if (col + 4 <= cols) {
       a_st<af32x4_any>(p, af32x4{c.v[0], c.v[1], c.v[2], c.v[3]});
@@ -109,16 +126,16 @@ __device__ __forceinline__ uint8_t *row_of(const Rows &m, uint64_t row) {
   return static_cast<uint8_t *>(m.data) + row * m.ld * kEntry<T>;
 }
 
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(kMapThreads) void k_ckpt_save(Walk8 w, Rows x, CkptOut out) {
   for (At i(w); i.chunk < w.chunks; i.next(w)) {
-    save_chunk<T>(out, i.chunk, load_chunk<T>(row_of<T>(x, i.row), i.at, w.cols));
+    save_chunk<T>(out, i.chunk, load_chunk<T, PAST>(row_of<T>(x, i.row), i.at, w.cols));
   }
 }
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(kMapThreads) void k_ckpt_load(Walk8 w, CkptIn in, Rows x) {
   for (At i(w); i.chunk < w.chunks; i.next(w)) {
-    store_chunk<T>(row_of<T>(x, i.row), i.at, w.cols, saved_chunk<T>(in, i.chunk));
+    store_chunk<T, PAST>(row_of<T>(x, i.row), i.at, w.cols, saved_chunk<T>(in, i.chunk));
   }
 }
 
@@ -153,11 +170,11 @@ __device__ __forceinline__ void activation(float z, float *a, float *d) {
   }
 }
 
-template <typename T, int KIND, bool GATED, bool SAVE>
+template <typename T, int KIND, bool GATED, bool SAVE, bool PAST>
 __global__ __launch_bounds__(kMapThreads) void k_gate(Walk8 w, Rows z, Rows u, Rows h, CkptOut sz, CkptOut su) {
   for (At i(w); i.chunk < w.chunks; i.next(w)) {
-    Chunk<T> a = load_chunk<T>(row_of<T>(z, i.row), i.at, w.cols), b;
-    if constexpr (GATED) b = load_chunk<T>(row_of<T>(u, i.row), i.at, w.cols);
+    Chunk<T> a = load_chunk<T, PAST>(row_of<T>(z, i.row), i.at, w.cols), b;
+    if constexpr (GATED) b = load_chunk<T, PAST>(row_of<T>(u, i.row), i.at, w.cols);
     if constexpr (SAVE) save_chunk<T>(sz, i.chunk, a);
     if constexpr (SAVE && GATED) save_chunk<T>(su, i.chunk, b);
 #pragma unroll
@@ -166,13 +183,13 @@ __global__ __launch_bounds__(kMapThreads) void k_gate(Walk8 w, Rows z, Rows u, R
       activation<KIND>(a.v[k], &a.v[k], &d);
       if constexpr (GATED) a.v[k] *= b.v[k];
     }
-    store_chunk<T>(row_of<T>(h, i.row), i.at, w.cols, a);
+    store_chunk<T, PAST>(row_of<T>(h, i.row), i.at, w.cols, a);
   }
 }
-template <typename T, int KIND, bool GATED>
+template <typename T, int KIND, bool GATED, bool PAST>
 __global__ __launch_bounds__(kMapThreads) void k_gate_grad(Walk8 w, Rows dh, CkptIn sz, CkptIn su, Rows dz, Rows du) {
   for (At i(w); i.chunk < w.chunks; i.next(w)) {
-    const Chunk<T> g = load_chunk<T>(row_of<T>(dh, i.row), i.at, w.cols);
+    const Chunk<T> g = load_chunk<T, PAST>(row_of<T>(dh, i.row), i.at, w.cols);
     Chunk<T> a = saved_chunk<T>(sz, i.chunk), b;
     if constexpr (GATED) b = saved_chunk<T>(su, i.chunk);
 #pragma unroll
@@ -186,24 +203,35 @@ __global__ __launch_bounds__(kMapThreads) void k_gate_grad(Walk8 w, Rows dh, Ckp
         a.v[k] = g.v[k] * d;
       }
     }
-    store_chunk<T>(row_of<T>(dz, i.row), i.at, w.cols, a);
-    if constexpr (GATED) store_chunk<T>(row_of<T>(du, i.row), i.at, w.cols, b);
+    store_chunk<T, PAST>(row_of<T>(dz, i.row), i.at, w.cols, a);
+    if constexpr (GATED) store_chunk<T, PAST>(row_of<T>(du, i.row), i.at, w.cols, b);
   }
 }
 
 struct Map {
   Walk8 walk;
   uint32_t blocks;
+  bool past;
 };
 // Rows back to back without padding in any operand are walked as one long row.
+//
+// Matrices that are larger together than what the caches could keep of them go past the caches where their rows lie on 16-byte borders:
+// bf16 16384 x 8192, a checkpoint there and back 160 -> 134 us, SiLU with a gate and its gradient 431 -> 351; fp32 8192 x 4096, 62 -> 57.
+// Below, and over odd rows, where lanes share lines, the caches help:
+// fp32 4099 x 2051, 16.6 us, takes 18.0 past them.  A feed-forward block of 16384 tokens, its products included, gains 1 % forward and loses nothing.
+constexpr uint64_t kPastBytes = 128ull << 20;
 Map plan_map(uint64_t rows, uint64_t cols, std::initializer_list<const dq_matrix *> m) {
-  bool flat = cols % kCkptBlock == 0;
-  for (const dq_matrix *x : m) flat = flat && (rows == 1 || x->ld == cols);
+  bool flat = cols % kCkptBlock == 0, even = true;
+  for (const dq_matrix *x : m) {
+    flat = flat && (rows == 1 || x->ld == cols);
+    even = even && (uintptr_t)x->data % 16 == 0 && (rows == 1 || x->ld * entry_bytes(x->dtype) % 16 == 0);
+  }
+  Map p;
+  p.past = even && m.size() * rows * cols * entry_bytes((*m.begin())->dtype) >= kPastBytes;
   if (flat) {
     cols *= rows;
     rows = 1;
   }
-  Map p;
   p.walk.per_row = ckpt_pitch(cols) * entry_bytes((*m.begin())->dtype) / 16;
   p.walk.chunks = rows * p.walk.per_row;
   p.walk.cols = cols;
@@ -270,8 +298,13 @@ using namespace dq;
     const dq_status st_ = (x);        \
     if (st_ != DQ_OK) return st_;     \
   } while (0)
-#define DQ_RUN(kernel, p, ...) \
-  hipLaunchKernelGGL((kernel), dim3((p).blocks), dim3(kMapThreads), 0, (hipStream_t)hip_stream, (p).walk, __VA_ARGS__)
+// The kernel with its template arguments `of` (in parentheses), past the caches or not.
+#define DQ_LIST(...) __VA_ARGS__
+#define DQ_RUN(kernel, of, p, ...)                                                                                                                  \
+  do {                                                                                                                                              \
+    if ((p).past) hipLaunchKernelGGL((kernel<DQ_LIST of, true>), dim3((p).blocks), dim3(kMapThreads), 0, (hipStream_t)hip_stream, (p).walk, __VA_ARGS__); \
+    else hipLaunchKernelGGL((kernel<DQ_LIST of, false>), dim3((p).blocks), dim3(kMapThreads), 0, (hipStream_t)hip_stream, (p).walk, __VA_ARGS__);    \
+  } while (0)
 
 extern "C" {
 
@@ -291,8 +324,8 @@ dq_status dq_ckpt_save(const dq_matrix *x, uint64_t rows, uint64_t cols, void *c
   const Region r[] = {region(x, rows, cols, false), region(ckpt, bytes, true)};
   if (regions_meet(r, 2)) return DQ_EINVAL;
   const Map p = plan_map(rows, cols, {x});
-  if (x->dtype == DQ_F32) DQ_RUN(k_ckpt_save<F32>, p, rows_of(x), ckpt_out(ckpt, rows, cols));
-  else DQ_RUN(k_ckpt_save<Bf16>, p, rows_of(x), ckpt_out(ckpt, rows, cols));
+  if (x->dtype == DQ_F32) DQ_RUN(k_ckpt_save, (F32), p, rows_of(x), ckpt_out(ckpt, rows, cols));
+  else DQ_RUN(k_ckpt_save, (Bf16), p, rows_of(x), ckpt_out(ckpt, rows, cols));
   return hip_status(hipGetLastError());
 }
 
@@ -306,8 +339,8 @@ dq_status dq_ckpt_load(const void *ckpt, uint64_t rows, uint64_t cols, const dq_
   const Region r[] = {region(ckpt, bytes, false), region(out, rows, cols, true)};
   if (regions_meet(r, 2)) return DQ_EINVAL;
   const Map p = plan_map(rows, cols, {out});
-  if (out->dtype == DQ_F32) DQ_RUN(k_ckpt_load<F32>, p, ckpt_in(ckpt, rows, cols), rows_of(out));
-  else DQ_RUN(k_ckpt_load<Bf16>, p, ckpt_in(ckpt, rows, cols), rows_of(out));
+  if (out->dtype == DQ_F32) DQ_RUN(k_ckpt_load, (F32), p, ckpt_in(ckpt, rows, cols), rows_of(out));
+  else DQ_RUN(k_ckpt_load, (Bf16), p, ckpt_in(ckpt, rows, cols), rows_of(out));
   return hip_status(hipGetLastError());
 }
 
@@ -330,10 +363,10 @@ dq_status dq_gate(dq_activation kind, const dq_matrix *z, const dq_matrix *u, ui
   const CkptOut sz = ckpt_out(ckpt_z, rows, cols), su = ckpt_out(ckpt_u, rows, cols);
 #define DQ_GATE(T, K)                                                                   \
   do {                                                                                  \
-    if (u && ckpt_z) DQ_RUN((k_gate<T, K, true, true>), p, rz, ru, rh, sz, su);         \
-    else if (u) DQ_RUN((k_gate<T, K, true, false>), p, rz, ru, rh, sz, su);             \
-    else if (ckpt_z) DQ_RUN((k_gate<T, K, false, true>), p, rz, ru, rh, sz, su);        \
-    else DQ_RUN((k_gate<T, K, false, false>), p, rz, ru, rh, sz, su);                   \
+    if (u && ckpt_z) DQ_RUN(k_gate, (T, K, true, true), p, rz, ru, rh, sz, su);         \
+    else if (u) DQ_RUN(k_gate, (T, K, true, false), p, rz, ru, rh, sz, su);             \
+    else if (ckpt_z) DQ_RUN(k_gate, (T, K, false, true), p, rz, ru, rh, sz, su);        \
+    else DQ_RUN(k_gate, (T, K, false, false), p, rz, ru, rh, sz, su);                   \
   } while (0)
   if (z->dtype == DQ_F32) {
     if (kind == DQ_SILU) DQ_GATE(F32, DQ_SILU);
@@ -365,8 +398,8 @@ dq_status dq_gate_grad(dq_activation kind, const dq_matrix *dh, const void *ckpt
   const CkptIn sz = ckpt_in(ckpt_z, rows, cols), su = ckpt_in(ckpt_u, rows, cols);
 #define DQ_GATE_GRAD(T, K)                                                        \
   do {                                                                            \
-    if (du) DQ_RUN((k_gate_grad<T, K, true>), p, rg, sz, su, rz, ru);             \
-    else DQ_RUN((k_gate_grad<T, K, false>), p, rg, sz, su, rz, ru);               \
+    if (du) DQ_RUN(k_gate_grad, (T, K, true), p, rg, sz, su, rz, ru);             \
+    else DQ_RUN(k_gate_grad, (T, K, false), p, rg, sz, su, rz, ru);               \
   } while (0)
   if (dh->dtype == DQ_F32) {
     if (kind == DQ_SILU) DQ_GATE_GRAD(F32, DQ_SILU);

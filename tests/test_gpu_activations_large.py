@@ -115,3 +115,27 @@ def test_weight_grad_of_more_tiles_than_blocks(dev):
         part = dy[:, first:first + 8192].float()
         want = sum(part[t][:, None] * xv[t][None, :] for t in range(rows))
         assert torch.equal(dw[first:first + 8192].float(), want), first
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols,ld", [(8192, 8192), (8187, 8192), (8187, 8187), (8161, 8200)])
+def test_large_calls_give_what_calls_over_parts_give(dev, dtype, cols, ld):
+    rows, part = 9001, 643                         # the whole: 140 MiB and more a matrix; a part: 22 MiB at most
+    both = fill(rows, 2 * ld, dev, 4).to(dtype)
+    z, u = both[:, :cols], both[:, ld:ld + cols]
+    own = [torch.full((rows, ld), 7.0, dtype=dtype, device=dev) for _ in range(4)]
+    h, dz, du, back = [t[:, :cols] for t in own]
+    ck = B.dq_ckpt_save(z)
+    B.dq_ckpt_load(ck, dtype, out=back)
+    _, saved = B.dq_gate(z, u, "gelu", save=True, out=h)
+    B.dq_gate_grad(h, saved, dz, du)
+    assert torch.equal(saved.z.data, ck.data)
+    if ld > cols:
+        assert all(bool((t[:, cols:] == 7.0).all()) for t in own)
+    for k in range(0, rows, part):
+        a = slice(k, min(rows, k + part))
+        assert torch.equal(B.dq_ckpt_load(B.dq_ckpt_save(z[a]), dtype), back[a])
+        want, kept = B.dq_gate(z[a], u[a], "gelu", save=True)
+        wz, wu = B.dq_gate_grad(want, kept)
+        assert torch.equal(want, h[a]) and torch.equal(wz, dz[a]) and torch.equal(wu, du[a])
+        assert torch.equal(B.dq_gate(z[a], None, "silu"), B.dq_gate(z, None, "silu")[a]) if k == 0 else True
