@@ -15,80 +15,24 @@ namespace {
 constexpr uint32_t kMapThreads = 256;
 
 // Here a lane's chunk is 16 bytes of a row, so that a wave's loads and stores each cover memory without gaps: 8 entries of bf16, 4 of
-// binary32 (with 8 of them, 32 bytes, half of each line a store touched came with the next one: 16384 x 4096, saved and loaded through the caches, took 174 us, not 146).
+// binary32 (with 8 of them, 32 bytes, half of each line a store touched came with the next one: 16384 x 4096, saved and loaded through
+// the caches, took 174 us, not 146).
 template <typename T>
 constexpr uint32_t kChunk = 16 / kEntry<T>;
 template <typename T>
 struct Chunk {
   float v[kChunk<T>];
 };
-// PAST: past the caches, in large calls (see plan_map).
 template <typename T, bool PAST>
 __device__ __forceinline__ Chunk<T> load_chunk(const void *row, uint64_t at, uint64_t cols) {
   Chunk<T> c;
-  const uint64_t col = at * kChunk<T>;
-  if (PAST && col + kChunk<T> <= cols) {
-    const a32x4 q = __builtin_nontemporal_load(static_cast<const __attribute__((address_space(1))) a32x4 *>((const __attribute__((address_space(1))) void *)row) + at);
-    if constexpr (__is_same(T, F32)) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c.v[i] = a_float(q[i]);
-    } else {
-      widen8<T>(Raw8<T>{{q}}, c.v);
-    }
-  } else if constexpr (__is_same(T, F32)) {
-    const uint8_t *p = static_cast<const uint8_t *>(row) + col * 4;
-    if (col + 4 <= cols) {
-      const af32x4 q = a_ld<af32x4_any>(p);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c.v[i] = q[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c.v[i] = col + i < cols ? a_ld<float>(p + 4 * i) : 0.0f;
-    }
-  } else {
-    load8<T>(row, col, cols, c.v);
-  }
+  widen(load_raw<T, kChunk<T>, PAST>(row, at * kChunk<T>, cols), c.v);
   return c;
-}
-template <typename T, bool PAST>
-__device__ __forceinline__ void store_chunk(void *row, uint64_t at, uint64_t cols, const Chunk<T> &c) {
-  const uint64_t col = at * kChunk<T>;
-  if (PAST && col + kChunk<T> <= cols) {
-    a32x4 q;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (__is_same(T, F32)) q[i] = a_bits(c.v[i]);
-      else q[i] = to_bf16x2(c.v[2 * i], c.v[2 * i + 1]);
-    }
-    __builtin_nontemporal_store(q, static_cast<__attribute__((address_space(1))) a32x4 *>((__attribute__((address_space(1))) void *)row) + at);
-  } else if constexpr (__is_same(T, F32)) {
-    uint8_t *p = static_cast<uint8_t *>(row) + col * 4;
-    if (col + 4 <= cols) {
-      a_st<af32x4_any>(p, af32x4{c.v[0], c.v[1], c.v[2], c.v[3]});
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (col + i < cols) a_st<float>(p + 4 * i, c.v[i]);
-    }
-  } else {
-    store8<T>(row, col, cols, c.v);
-  }
-}
-// Chunk number n of a checkpoint.
-template <typename T>
-__device__ __forceinline__ void save_chunk(const CkptOut &out, uint64_t n, const Chunk<T> &c) {
-  constexpr uint32_t lanes = kCkptBlock / kChunk<T>;
-  uint32_t scale;
-  auto codes = ckpt_encode(c.v, &scale);
-  a_st<decltype(codes)>(out.codes + n * kChunk<T>, codes);
-  if (n % lanes == 0) a_st<uint8_t>(out.scales + n / lanes, (uint8_t)scale);
 }
 template <typename T>
 __device__ __forceinline__ Chunk<T> saved_chunk(const CkptIn &in, uint64_t n) {
   Chunk<T> c;
-  const uint32_t scale = a_ld<uint8_t>(in.scales + n / (kCkptBlock / kChunk<T>));
-  if constexpr (__is_same(T, F32)) ckpt_decode(a_ld<uint32_t>(in.codes + n * 4), scale, c.v);
-  else ckpt_decode(a_ld<a32x2>(in.codes + n * 8), scale, c.v);
+  ckpt_load(in, n, c.v);
   return c;
 }
 
@@ -129,13 +73,13 @@ __device__ __forceinline__ uint8_t *row_of(const Rows &m, uint64_t row) {
 template <typename T, bool PAST>
 __global__ __launch_bounds__(kMapThreads) void k_ckpt_save(Walk8 w, Rows x, CkptOut out) {
   for (At i(w); i.chunk < w.chunks; i.next(w)) {
-    save_chunk<T>(out, i.chunk, load_chunk<T, PAST>(row_of<T>(x, i.row), i.at, w.cols));
+    ckpt_store(out, i.chunk, load_chunk<T, PAST>(row_of<T>(x, i.row), i.at, w.cols).v);
   }
 }
 template <typename T, bool PAST>
 __global__ __launch_bounds__(kMapThreads) void k_ckpt_load(Walk8 w, CkptIn in, Rows x) {
   for (At i(w); i.chunk < w.chunks; i.next(w)) {
-    store_chunk<T, PAST>(row_of<T>(x, i.row), i.at, w.cols, saved_chunk<T>(in, i.chunk));
+    store_entries<T, kChunk<T>, PAST>(row_of<T>(x, i.row), i.at * kChunk<T>, w.cols, saved_chunk<T>(in, i.chunk).v);
   }
 }
 
@@ -175,15 +119,15 @@ __global__ __launch_bounds__(kMapThreads) void k_gate(Walk8 w, Rows z, Rows u, R
   for (At i(w); i.chunk < w.chunks; i.next(w)) {
     Chunk<T> a = load_chunk<T, PAST>(row_of<T>(z, i.row), i.at, w.cols), b;
     if constexpr (GATED) b = load_chunk<T, PAST>(row_of<T>(u, i.row), i.at, w.cols);
-    if constexpr (SAVE) save_chunk<T>(sz, i.chunk, a);
-    if constexpr (SAVE && GATED) save_chunk<T>(su, i.chunk, b);
+    if constexpr (SAVE) ckpt_store(sz, i.chunk, a.v);
+    if constexpr (SAVE && GATED) ckpt_store(su, i.chunk, b.v);
 #pragma unroll
     for (uint32_t k = 0; k < kChunk<T>; ++k) {
       float d;
       activation<KIND>(a.v[k], &a.v[k], &d);
       if constexpr (GATED) a.v[k] *= b.v[k];
     }
-    store_chunk<T, PAST>(row_of<T>(h, i.row), i.at, w.cols, a);
+    store_entries<T, kChunk<T>, PAST>(row_of<T>(h, i.row), i.at * kChunk<T>, w.cols, a.v);
   }
 }
 template <typename T, int KIND, bool GATED, bool PAST>
@@ -203,8 +147,8 @@ __global__ __launch_bounds__(kMapThreads) void k_gate_grad(Walk8 w, Rows dh, Ckp
         a.v[k] = g.v[k] * d;
       }
     }
-    store_chunk<T, PAST>(row_of<T>(dz, i.row), i.at, w.cols, a);
-    if constexpr (GATED) store_chunk<T, PAST>(row_of<T>(du, i.row), i.at, w.cols, b);
+    store_entries<T, kChunk<T>, PAST>(row_of<T>(dz, i.row), i.at * kChunk<T>, w.cols, a.v);
+    if constexpr (GATED) store_entries<T, kChunk<T>, PAST>(row_of<T>(du, i.row), i.at * kChunk<T>, w.cols, b.v);
   }
 }
 
@@ -215,16 +159,14 @@ struct Map {
 };
 // Rows back to back without padding in any operand are walked as one long row.
 //
-// Matrices that are larger together than what the caches could keep of them go past the caches where their rows lie on 16-byte borders:
-// bf16 16384 x 8192, a checkpoint there and back 160 -> 134 us, SiLU with a gate and its gradient 431 -> 351; fp32 8192 x 4096, 62 -> 57.
+// Large matrices go past the caches: bf16 16384 x 8192, a checkpoint there and back 160 -> 134 us, SiLU with a gate and its gradient 431 -> 351; fp32 8192 x 4096, 62 -> 57.
 // Below, and over odd rows, where lanes share lines, the caches help:
 // fp32 4099 x 2051, 16.6 us, takes 18.0 past them.  A feed-forward block of 16384 tokens, its products included, gains 1 % forward and loses nothing.
-constexpr uint64_t kPastBytes = 128ull << 20;
 Map plan_map(uint64_t rows, uint64_t cols, std::initializer_list<const dq_matrix *> m) {
   bool flat = cols % kCkptBlock == 0, even = true;
   for (const dq_matrix *x : m) {
     flat = flat && (rows == 1 || x->ld == cols);
-    even = even && (uintptr_t)x->data % 16 == 0 && (rows == 1 || x->ld * entry_bytes(x->dtype) % 16 == 0);
+    even = even && on_16(x, rows);
   }
   Map p;
   p.past = even && m.size() * rows * cols * entry_bytes((*m.begin())->dtype) >= kPastBytes;

@@ -1,10 +1,12 @@
 // Rows of activations as the checkpoint, layer norm, gate and weight-gradient kernels read and write them, and the checkpoint's
 // 8-bit blocks.
 //
-// A row is cut into chunks of 8 entries, one lane's share; four neighbouring lanes hold a block of 32.  Rows start at any multiple
+// A row is cut into chunks, one lane's share; the neighbouring lanes of a block of 32 hold it together.  Rows start at any multiple
 // of the entry size: gfx950 loads and stores 16 bytes from any address, at full rate where they do not cross a cache line, so
 // there is one path for every stride, and only a row's last chunk may have to go entry by entry.
 #pragma once
+#include <type_traits>
+
 #include "dq_device.h"
 
 namespace dq {
@@ -46,22 +48,30 @@ struct Bf16 {};
 template <typename T>
 constexpr uint32_t kEntry = __is_same(T, F32) ? 4 : 2;
 
-// Eight entries as they lie in memory.
-template <typename T>
-struct Raw8 {
-  a32x4 w[kEntry<T> / 2];
+// Two binary32 numbers as bf16, rounded to nearest even.
+__device__ __forceinline__ uint32_t to_bf16x2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(af32x2{a, b}, bf16x2));
+}
+// N entries of a row, 16 bytes or 32, as they lie in memory.
+template <typename T, uint32_t N>
+struct Raw {
+  a32x4 w[N * kEntry<T> / 16];
 };
-// Entries col .. col + 7 of the row at `row`, of which `cols` exist; the others are zero.
-template <typename T>
-__device__ __forceinline__ Raw8<T> load_raw8(const void *row, uint64_t col, uint64_t cols) {
+// Entries col .. col + N - 1 of the row at `row`, of which `cols` exist; the others are zero.  PAST: past the caches, for rows on
+// 16-byte borders.
+template <typename T, uint32_t N, bool PAST = false>
+__device__ __forceinline__ Raw<T, N> load_raw(const void *row, uint64_t col, uint64_t cols) {
   const uint8_t *p = static_cast<const uint8_t *>(row) + col * kEntry<T>;
-  Raw8<T> r;
-  if (col + 8 <= cols) {
-    r.w[0] = a_ld<a32x4_any>(p);
-    if constexpr (__is_same(T, F32)) r.w[1] = a_ld<a32x4_any>(p + 16);
+  Raw<T, N> r;
+  if (col + N <= cols) {
+#pragma unroll
+    for (uint32_t q = 0; q < N * kEntry<T> / 16; ++q) {
+      if constexpr (PAST) r.w[q] = __builtin_nontemporal_load((const __attribute__((address_space(1))) a32x4 *)(p + 16 * q));
+      else r.w[q] = a_ld<a32x4_any>(p + 16 * q);
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < (int)kEntry<T> * 2; ++i) {
+    for (int i = 0; i < (int)(N * kEntry<T> / 4); ++i) {
       uint32_t v = 0;
       if constexpr (__is_same(T, F32)) {
         if (col + i < cols) v = a_ld<uint32_t>(p + 4 * i);
@@ -74,49 +84,59 @@ __device__ __forceinline__ Raw8<T> load_raw8(const void *row, uint64_t col, uint
   }
   return r;
 }
-template <typename T>
-__device__ __forceinline__ void widen8(const Raw8<T> &r, float (&v)[8]) {
+template <typename T, uint32_t N>
+__device__ __forceinline__ void widen(const Raw<T, N> &r, float (&v)[N]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (uint32_t i = 0; i < N * kEntry<T> / 4; ++i) {
+    const uint32_t w = r.w[i / 4][i % 4];
     if constexpr (__is_same(T, F32)) {
-      v[i] = a_float(r.w[0][i]);
-      v[4 + i] = a_float(r.w[1][i]);
+      v[i] = a_float(w);
     } else {
-      v[2 * i] = a_float(r.w[0][i] << 16);
-      v[2 * i + 1] = a_float(r.w[0][i] & 0xFFFF0000u);
+      v[2 * i] = a_float(w << 16);
+      v[2 * i + 1] = a_float(w & 0xFFFF0000u);
     }
+  }
+}
+template <typename T, uint32_t N>
+__device__ __forceinline__ void load_entries(const void *row, uint64_t col, uint64_t cols, float (&v)[N]) {
+  if constexpr (N * kEntry<T> >= 16) {
+    widen(load_raw<T, N>(row, col, cols), v);
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) v[i] = col + i < cols ? a_float((uint32_t)a_ld<uint16_t>(static_cast<const uint8_t *>(row) + (col + i) * 2) << 16) : 0.0f;
+  }
+}
+template <typename T, uint32_t N, bool PAST = false>
+__device__ __forceinline__ void store_entries(void *row, uint64_t col, uint64_t cols, const float (&v)[N]) {
+  uint8_t *p = static_cast<uint8_t *>(row) + col * kEntry<T>;
+  Raw<T, N> r;
+#pragma unroll
+  for (uint32_t i = 0; i < N * kEntry<T> / 4; ++i) {
+    if constexpr (__is_same(T, F32)) r.w[i / 4][i % 4] = a_bits(v[i]);
+    else r.w[i / 4][i % 4] = to_bf16x2(v[2 * i], v[2 * i + 1]);
+  }
+  if (col + N <= cols) {
+#pragma unroll
+    for (uint32_t q = 0; q < N * kEntry<T> / 16; ++q) {
+      if constexpr (PAST) __builtin_nontemporal_store(r.w[q], (__attribute__((address_space(1))) a32x4 *)(p + 16 * q));
+      else a_st<a32x4_any>(p + 16 * q, r.w[q]);
+    }
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i)
+      if (col + i < cols) {
+        if constexpr (__is_same(T, F32)) a_st<uint32_t>(p + 4 * i, r.w[i / 4][i % 4]);
+        else a_st<uint16_t>(p + 2 * i, (uint16_t)(r.w[i / 8][i / 2 % 4] >> (16 * (i % 2))));
+      }
   }
 }
 template <typename T>
 __device__ __forceinline__ void load8(const void *row, uint64_t col, uint64_t cols, float (&v)[8]) {
-  widen8<T>(load_raw8<T>(row, col, cols), v);
-}
-// Two binary32 numbers as bf16, rounded to nearest even.
-__device__ __forceinline__ uint32_t to_bf16x2(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(af32x2{a, b}, bf16x2));
+  load_entries<T, 8>(row, col, cols, v);
 }
 template <typename T>
 __device__ __forceinline__ void store8(void *row, uint64_t col, uint64_t cols, const float (&v)[8]) {
-  uint8_t *p = static_cast<uint8_t *>(row) + col * kEntry<T>;
-  if constexpr (__is_same(T, F32)) {
-    if (col + 8 <= cols) {
-      a_st<af32x4_any>(p, af32x4{v[0], v[1], v[2], v[3]});
-      a_st<af32x4_any>(p + 16, af32x4{v[4], v[5], v[6], v[7]});
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (col + i < cols) a_st<float>(p + 4 * i, v[i]);
-    }
-  } else {
-    const a32x4 w = {to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
-    if (col + 8 <= cols) {
-      a_st<a32x4_any>(p, w);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (col + i < cols) a_st<uint16_t>(p + 2 * i, (uint16_t)(w[i / 2] >> (16 * (i % 2))));
-    }
-  }
+  store_entries<T, 8>(row, col, cols, v);
 }
 
 // The largest of the four lanes of a block.
@@ -168,7 +188,9 @@ __device__ __forceinline__ void ckpt_decode(uint32_t codes, uint32_t scale, floa
   const af32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, X, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, X, true);
   v[0] = lo.x; v[1] = lo.y; v[2] = hi.x; v[3] = hi.y;
 }
-// Chunk number `chunk` of a checkpoint (its rows back to back, each pitch / 8 chunks): codes at 8 * chunk, its block's scale behind them.
+// The codes of a chunk of N entries as they lie in memory.
+template <uint32_t N>
+using CkptCodes = std::conditional_t<N == 8, a32x2, uint32_t>;
 struct CkptIn {
   const uint8_t *codes, *scales;
 };
@@ -183,14 +205,18 @@ inline CkptOut ckpt_out(void *p, uint64_t rows, uint64_t cols) {
   if (!p) return {nullptr, nullptr};
   return {static_cast<uint8_t *>(p), static_cast<uint8_t *>(p) + rows * ckpt_pitch(cols)};
 }
-__device__ __forceinline__ void ckpt_load8(const CkptIn &c, uint64_t chunk, float (&v)[8]) {
-  ckpt_decode(a_ld<a32x2>(c.codes + chunk * 8), a_ld<uint8_t>(c.scales + chunk / 4), v);
+// Chunk number `chunk` of a checkpoint (its rows back to back, each pitch / N chunks): its codes, and its block's scale behind all codes.
+// All lanes of a block save together.
+template <uint32_t N>
+__device__ __forceinline__ void ckpt_load(const CkptIn &c, uint64_t chunk, float (&v)[N]) {
+  ckpt_decode(a_ld<CkptCodes<N>>(c.codes + chunk * N), a_ld<uint8_t>(c.scales + chunk / (kCkptBlock / N)), v);
 }
-__device__ __forceinline__ void ckpt_store8(const CkptOut &c, uint64_t chunk, const float (&v)[8]) {
+template <uint32_t N>
+__device__ __forceinline__ void ckpt_store(const CkptOut &c, uint64_t chunk, const float (&v)[N]) {
   uint32_t scale;
-  const a32x2 codes = ckpt_encode(v, &scale);
-  a_st<a32x2>(c.codes + chunk * 8, codes);
-  if (chunk % 4 == 0) a_st<uint8_t>(c.scales + chunk / 4, (uint8_t)scale);
+  const CkptCodes<N> codes = ckpt_encode(v, &scale);
+  a_st<CkptCodes<N>>(c.codes + chunk * N, codes);
+  if (chunk % (kCkptBlock / N) == 0) a_st<uint8_t>(c.scales + chunk / (kCkptBlock / N), (uint8_t)scale);
 }
 
 // Host side: what the entry points check.
@@ -204,6 +230,10 @@ inline Region region(const dq_matrix *m, uint64_t rows, uint64_t cols, bool writ
   const uint64_t e = entry_bytes(m->dtype);
   return {m->data, rows, cols * e, rows > 1 ? m->ld * e : cols * e, written};
 }
+// Matrices of one call that together are larger than what the caches could keep of them go past the caches, where their rows lie on
+// 16-byte borders.
+constexpr uint64_t kPastBytes = 128ull << 20;
+inline bool on_16(const dq_matrix *m, uint64_t rows) { return (uintptr_t)m->data % 16 == 0 && (rows == 1 || m->ld * entry_bytes(m->dtype) % 16 == 0); }
 // Whether some written region meets another one.
 bool regions_meet(const Region *r, int n);
 // A matrix that a call may read or write: DQ_OK, DQ_EINVAL or DQ_EALIGN.

@@ -60,13 +60,14 @@ struct NormIn {
   uint32_t bf16;              // whether they are bf16
   float eps;
 };
-__device__ __forceinline__ void weight8(const void *w, uint32_t bf16, uint64_t col, uint64_t cols, float otherwise, float (&v)[8]) {
+template <uint32_t N>
+__device__ __forceinline__ void weights_at(const void *w, uint32_t bf16, uint64_t col, uint64_t cols, float otherwise, float (&v)[N]) {
   if (w) {
-    if (bf16) load8<Bf16>(w, col, cols, v);
-    else load8<F32>(w, col, cols, v);
+    if (bf16) load_entries<Bf16, N>(w, col, cols, v);
+    else load_entries<F32, N>(w, col, cols, v);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = otherwise;
+    for (uint32_t i = 0; i < N; ++i) v[i] = otherwise;
   }
 }
 
@@ -74,14 +75,22 @@ __device__ __forceinline__ void weight8(const void *w, uint32_t bf16, uint64_t c
 // KEEP chunks of 8 entries each.  A row goes to one wave where that is enough (up to 2,048 entries) and there are rows for all, so that
 // its sums need no barrier; a wave has two or four of the short rows (up to 256 and 128 entries).  The next row is loaded while one
 // is worked on, and there are as many blocks as stay resident, so that most rows are loaded so.
-// Measured (forward and backward, 5.2 TB/s being a large copy's rate): bf16 16384 x 2048 72 us (4.7 TB/s), 200000 x 128 59 us (4.3),
-// 16384 x 4096 135 us (5.0), 4096 x 16384 169 us (4.0); fp32 1021 x 6151 38 us (3.0).
+// Measured (forward and backward, 5.2 TB/s being a large copy's rate): bf16 16384 x 2048 69 us (4.9 TB/s), 200000 x 128 57 us (4.5),
+// 65536 x 2048 228 us (5.9), 16384 x 4096 129 us (5.2), 4096 x 16384 159 us (4.2); fp32 16384 x 4096 207 us (5.8), 1021 x 6151 37 us (3.1).
+//
+// PAST: rows of large calls go past the caches.  A wave's loads and stores then have to cover memory without gaps, so a chunk is 16 bytes,
+// twice as many of 4 entries in fp32.  Forward and backward, through the caches and past them: bf16 65536 x 2048 265 and 228 us,
+// 16384 x 4096 136 and 128, fp32 16384 x 4096 231 and 207.  Below, chunks of 8 are as good or better (fp32 1024 x 8192 41 and 43), and
+// better over odd rows (fp32 3000 x 7001 96, 105 with 4).  The forward pass takes twice the size for large (bf16 16384 x 2048 by itself
+// 21.9 and 24.3 us: the matrix that it reads may still be in the caches).
 //
 // A block's groups take a row each, the block then the next rows; all of them come round as often as each other.
-template <uint32_t GROUP, uint32_t KEEP>
+template <typename T, uint32_t GROUP, uint32_t KEEP, bool PAST>
 struct Fit {
-  static constexpr uint32_t kGroup = GROUP, kKeep = KEEP;
-  static constexpr bool kAheadBackward = GROUP <= 64 || KEEP <= 3;  // with more, the backward pass has no registers to load ahead
+  typedef T Type;
+  static constexpr uint32_t kEntries = PAST ? 16 / kEntry<T> : 8;  // of a chunk
+  static constexpr uint32_t kGroup = GROUP, kEights = KEEP, kKeep = KEEP * 8 / kEntries;
+  static constexpr bool kPast = PAST, kAheadBackward = GROUP <= 64 || KEEP <= 3;  // with more, the backward pass has no registers to load ahead
   static constexpr uint32_t kBlock = 512, kGroups = kBlock / GROUP;  // of the backward pass
 };
 // Sums of a and b over a group, in all its threads; the order is fixed.  All threads of the block come here.
@@ -105,59 +114,62 @@ __device__ __forceinline__ void group_sums(float &a, float &b, af32x2 *lds) {
   }
 }
 
-// A weight (or a bias) as the threads of a group read it, eight entries at a time: from registers, or, where a wave has a row and many
+// A weight (or a bias) as the threads of a group read it, a chunk at a time: from registers, or, where a wave has a row and many
 // rows pass, from LDS, which leaves registers for the next row.
 template <typename F>
 struct Weight {
+  typedef __attribute__((address_space(3))) af32x4 lds_quad;
   static constexpr bool kInLds = F::kGroup <= 64;
-  static constexpr uint32_t kChunks = F::kGroup * F::kKeep, kLds = kInLds ? kChunks * 8 : 4;  // floats
-  float v[kInLds ? 1 : F::kKeep][8];
+  static constexpr uint32_t N = F::kEntries, kChunks = F::kGroup * F::kKeep, kLds = kInLds ? kChunks * N : 4;  // floats
+  float v[kInLds ? 1 : F::kKeep][N];
   uint32_t lds;
   __device__ __forceinline__ Weight(const void *w, uint32_t bf16, uint32_t cols, float otherwise, float *buffer)
       : lds((uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)buffer) {
     if constexpr (!kInLds) {
 #pragma unroll
-      for (uint32_t k = 0; k < F::kKeep; ++k) weight8(w, bf16, (threadIdx.x % F::kGroup + k * F::kGroup) * 8, cols, otherwise, v[k]);
-    } else {  // the chunks' first halves, then their second ones: 16 bytes a lane, side by side
+      for (uint32_t k = 0; k < F::kKeep; ++k) weights_at(w, bf16, (threadIdx.x % F::kGroup + k * F::kGroup) * N, cols, otherwise, v[k]);
+    } else {  // the chunks' first four, then their second ones: 16 bytes a lane, side by side
       for (uint32_t c = threadIdx.x; c < kChunks; c += blockDim.x) {
-        float u[8];
-        weight8(w, bf16, c * 8, cols, otherwise, u);
-        put(c, u[0], u[1], u[2], u[3]);
-        put(kChunks + c, u[4], u[5], u[6], u[7]);
+        float u[N];
+        weights_at(w, bf16, c * N, cols, otherwise, u);
+#pragma unroll
+        for (uint32_t h = 0; h < N / 4; ++h) *reinterpret_cast<lds_quad *>(lds + (h * kChunks + c) * 16) = af32x4{u[4 * h], u[4 * h + 1], u[4 * h + 2], u[4 * h + 3]};
       }
     }
   }
-  typedef __attribute__((address_space(3))) af32x4 lds_quad;
-  __device__ __forceinline__ void put(uint32_t i, float a, float b, float c, float d) const { *reinterpret_cast<lds_quad *>(lds + i * 16) = af32x4{a, b, c, d}; }
-  __device__ __forceinline__ void get(uint32_t k, uint32_t chunk, float (&u)[8]) const {
+  __device__ __forceinline__ void get(uint32_t k, uint32_t chunk, float (&u)[N]) const {
     if constexpr (kInLds) {
-      const af32x4 a = *reinterpret_cast<const lds_quad *>(lds + chunk * 16), b = *reinterpret_cast<const lds_quad *>(lds + (kChunks + chunk) * 16);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { u[i] = a[i]; u[4 + i] = b[i]; }
+      for (uint32_t h = 0; h < N / 4; ++h) {
+        const af32x4 a = *reinterpret_cast<const lds_quad *>(lds + (h * kChunks + chunk) * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[4 * h + i] = a[i];
+      }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = v[k][i];
+      for (uint32_t i = 0; i < N; ++i) u[i] = v[k][i];
     }
   }
 };
 
-template <typename T, typename F>
+template <typename F>
 __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(NormIn in, Rows y, CkptOut saved, float *mean, float *rstd) {
-  constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
+  typedef typename F::Type T;
+  constexpr uint32_t N = F::kEntries, kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
   __shared__ af32x2 lds[kBlock / 64];
   __shared__ __attribute__((aligned(16))) float weights[2][Weight<F>::kLds];
-  const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, cols = (uint32_t)in.cols;
+  const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / N), me = threadIdx.x % F::kGroup, cols = (uint32_t)in.cols;
   const float inv = 1.0f / (float)in.cols;
   const Weight<F> w(in.weight, in.bf16, cols, 1.0f, weights[0]), b(in.bias, in.bf16, cols, 0.0f, weights[1]);
   if constexpr (Weight<F>::kInLds) __syncthreads();
-  Raw8<T> next[F::kKeep];
+  Raw<T, N> next[F::kKeep];
   auto load = [&](uint64_t r) {
     const uint8_t *x = static_cast<const uint8_t *>(in.x.data) + r * in.x.ld * kEntry<T>;
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
       const uint32_t c = me + k * F::kGroup;
-      next[k] = Raw8<T>{};
-      if (r < in.rows && c < chunks) next[k] = load_raw8<T>(x, c * 8, cols);
+      next[k] = Raw<T, N>{};
+      if (r < in.rows && c < chunks) next[k] = load_raw<T, N, F::kPast>(x, c * N, cols);
     }
   };
   const uint64_t step = (uint64_t)gridDim.x * kGroups;
@@ -165,30 +177,30 @@ __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(Norm
   load(r);
   for (uint64_t first = (uint64_t)blockIdx.x * kGroups; first < in.rows; first += step, r += step) {
     const bool here = r < in.rows;
-    float v[F::kKeep][8], s = 0.0f, none = 0.0f;
+    float v[F::kKeep][N], s = 0.0f, none = 0.0f;
 #pragma unroll
-    for (uint32_t k = 0; k < F::kKeep; ++k) widen8<T>(next[k], v[k]);
+    for (uint32_t k = 0; k < F::kKeep; ++k) widen(next[k], v[k]);
     load(r + step);
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s += v[k][i];
+      for (int i = 0; i < (int)N; ++i) s += v[k][i];
     group_sums<F::kGroup>(s, none, lds);
     const float m = s * inv;
     s = none = 0.0f;
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
-      int left = (int)cols - (int)((me + k * F::kGroup) * 8);  // of the row from this chunk on
+      int left = (int)cols - (int)((me + k * F::kGroup) * N);  // of the row from this chunk on
       asm volatile("" : "+v"(left));                            // (compared here, not in front of the loop, which would take 64 masks)
-      if (left >= 8) {
+      if (left >= (int)N) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < (int)N; ++i) {
           const float d = v[k][i] - m;
           s = fmaf(d, d, s);
         }
       } else if (left > 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < (int)N; ++i) {
           const float d = i < left ? v[k][i] - m : 0.0f;
           s = fmaf(d, d, s);
         }
@@ -201,13 +213,13 @@ __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(Norm
     for (uint32_t k = 0; k < F::kKeep; ++k) {
       const uint32_t c = me + k * F::kGroup;
       if (c >= chunks) continue;
-      if (saved.codes) ckpt_store8(saved, r * chunks + c, v[k]);
-      float wk[8], bk[8];
+      if (saved.codes) ckpt_store(saved, r * chunks + c, v[k]);
+      float wk[N], bk[N];
       w.get(k, c, wk);
       b.get(k, c, bk);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[k][i] = fmaf((v[k][i] - m) * scale, wk[i], bk[i]);
-      store8<T>(static_cast<uint8_t *>(y.data) + r * y.ld * kEntry<T>, c * 8, cols, v[k]);
+      for (int i = 0; i < (int)N; ++i) v[k][i] = fmaf((v[k][i] - m) * scale, wk[i], bk[i]);
+      store_entries<T, N, F::kPast>(static_cast<uint8_t *>(y.data) + r * y.ld * kEntry<T>, c * N, cols, v[k]);
     }
     if (me == 0 && mean) {
       mean[r] = m;
@@ -246,9 +258,9 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_wide(NormIn in, Rows y, C
     for (uint64_t c = threadIdx.x; c < chunks; c += kWideThreads) {
       float w[8], b[8];
       load8<T>(x, c * 8, in.cols, v);
-      if (saved.codes) ckpt_store8(saved, r * chunks + c, v);
-      weight8(in.weight, in.bf16, c * 8, in.cols, 1.0f, w);
-      weight8(in.bias, in.bf16, c * 8, in.cols, 0.0f, b);
+      if (saved.codes) ckpt_store(saved, r * chunks + c, v);
+      weights_at(in.weight, in.bf16, c * 8, in.cols, 1.0f, w);
+      weights_at(in.bias, in.bf16, c * 8, in.cols, 0.0f, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = fmaf((v[i] - m) * k, w[i], b[i]);
       store8<T>(static_cast<uint8_t *>(y.data) + r * y.ld * kEntry<T>, c * 8, in.cols, v);
@@ -272,22 +284,24 @@ struct NormGrad {
 // The backward pass of rows that stay in registers, with the sums over rows beside: a thread's columns are the same in all of its
 // rows, so it sums them up as they pass; at the end the block's groups add up and the block's sums go to `part`
 // ([blocks][2][pitch]).  One block of 512 threads to a CU (8 waves have what it takes in flight), so that there are few.
-template <typename T, typename F>
+template <typename F>
 __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *part) {
+  typedef typename F::Type T;
+  constexpr uint32_t N = F::kEntries;
   constexpr bool kAhead = F::kAheadBackward;
   __shared__ af32x2 lds[F::kBlock / 64];
-  __shared__ __attribute__((aligned(16))) float weights[Weight<F>::kLds], sums[F::kGroups > 1 ? F::kGroups / 2 * F::kGroup * F::kKeep * 16 : 4];
-  const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / 8), me = threadIdx.x % F::kGroup, group = threadIdx.x / F::kGroup, cols = (uint32_t)in.cols;
+  __shared__ __attribute__((aligned(16))) float weights[Weight<F>::kLds], sums[F::kGroups > 1 ? F::kGroups / 2 * F::kGroup * F::kKeep * N * 2 : 4];
+  const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / N), me = threadIdx.x % F::kGroup, group = threadIdx.x / F::kGroup, cols = (uint32_t)in.cols;
   const float inv = 1.0f / (float)in.cols;
   const Weight<F> w(in.weight, in.bf16, cols, 1.0f, weights);
   if constexpr (Weight<F>::kInLds) __syncthreads();
-  float dw[F::kKeep][8], db[F::kKeep][8];
+  float dw[F::kKeep][N], db[F::kKeep][N];
 #pragma unroll
   for (uint32_t k = 0; k < F::kKeep; ++k)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dw[k][i] = db[k][i] = 0.0f;
-  Raw8<T> next[F::kKeep];
-  a32x2 codes[F::kKeep];
+    for (int i = 0; i < (int)N; ++i) dw[k][i] = db[k][i] = 0.0f;
+  Raw<T, N> next[F::kKeep];
+  CkptCodes<N> codes[F::kKeep];
   uint32_t scales[F::kKeep];
   float next_m, next_scale;
   auto load = [&](uint64_t r) {
@@ -301,13 +315,13 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
       const uint32_t c = me + k * F::kGroup;
-      next[k] = Raw8<T>{};
-      codes[k] = a32x2{0u, 0u};
+      next[k] = Raw<T, N>{};
+      codes[k] = CkptCodes<N>{};
       scales[k] = kCkptLeast;
       if (here && c < chunks) {
-        next[k] = load_raw8<T>(dy, c * 8, cols);
-        codes[k] = a_ld<a32x2>(in.x.codes + (r * chunks + c) * 8);
-        scales[k] = a_ld<uint8_t>(in.x.scales + (r * chunks + c) / 4);
+        next[k] = load_raw<T, N, F::kPast>(dy, c * N, cols);
+        codes[k] = a_ld<CkptCodes<N>>(in.x.codes + (r * chunks + c) * N);
+        scales[k] = a_ld<uint8_t>(in.x.scales + (r * chunks + c) / (kCkptBlock / N));
       }
     }
   };
@@ -317,20 +331,20 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
   for (uint64_t first = (uint64_t)blockIdx.x * F::kGroups; first < in.rows; first += step, r += step) {
     const bool here = r < in.rows;
     if (!kAhead) load(r);
-    float g[F::kKeep][8], n[F::kKeep][8], s = 0.0f, sn = 0.0f;
+    float g[F::kKeep][N], n[F::kKeep][N], s = 0.0f, sn = 0.0f;
     const float m = next_m, scale = next_scale;
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
-      widen8<T>(next[k], g[k]);
+      widen(next[k], g[k]);
       ckpt_decode(codes[k], scales[k], n[k]);
     }
     if (kAhead) load(r + step);
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
-      float wk[8];
+      float wk[N];
       w.get(k, me + k * F::kGroup, wk);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < (int)N; ++i) {
         n[k][i] = (n[k][i] - m) * scale;
         dw[k][i] = fmaf(g[k][i], n[k][i], dw[k][i]);
         db[k][i] += g[k][i];
@@ -348,15 +362,15 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
       const uint32_t c = me + k * F::kGroup;
       if (c >= chunks) continue;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[k][i] = scale * ((g[k][i] - s) - n[k][i] * sn);
-      store8<T>(static_cast<uint8_t *>(in.dx.data) + r * in.dx.ld * kEntry<T>, c * 8, cols, g[k]);
+      for (int i = 0; i < (int)N; ++i) g[k][i] = scale * ((g[k][i] - s) - n[k][i] * sn);
+      store_entries<T, N, F::kPast>(static_cast<uint8_t *>(in.dx.data) + r * in.dx.ld * kEntry<T>, c * N, cols, g[k]);
     }
   }
   if (!part) return;
-  float *out = part + (uint64_t)blockIdx.x * 2 * chunks * 8;
+  float *out = part + (uint64_t)blockIdx.x * 2 * chunks * N;
   // The upper half of the groups leaves its sums in LDS, the lower half adds them, until one group has them all.
   typedef __attribute__((address_space(3))) af32x4 lds_quad;
-  constexpr uint32_t kSlot = F::kGroup * F::kKeep * 4;  // quads of a group's sums, in four parts: 16 bytes a lane, side by side
+  constexpr uint32_t kSlot = F::kGroup * F::kKeep * N / 2;  // quads of a group's sums, dw's then db's, as the weights lie: 16 bytes a lane, side by side
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)sums + me * 16;
 #pragma unroll
   for (uint32_t half = F::kGroups / 2; half; half /= 2) {
@@ -366,7 +380,7 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
 #pragma unroll
       for (uint32_t k = 0; k < F::kKeep; ++k)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < (int)N / 4; ++h) {
           lds_quad *at = reinterpret_cast<lds_quad *>(slot + (h * F::kKeep + k) * (F::kGroup * 16));
           *at = af32x4{dw[k][4 * h], dw[k][4 * h + 1], dw[k][4 * h + 2], dw[k][4 * h + 3]};
           at[kSlot / 2] = af32x4{db[k][4 * h], db[k][4 * h + 1], db[k][4 * h + 2], db[k][4 * h + 3]};
@@ -377,7 +391,7 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
 #pragma unroll
       for (uint32_t k = 0; k < F::kKeep; ++k)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < (int)N / 4; ++h) {
           const lds_quad *at = reinterpret_cast<const lds_quad *>(slot + (h * F::kKeep + k) * (F::kGroup * 16));
           const af32x4 a = *at, b = at[kSlot / 2];
 #pragma unroll
@@ -395,9 +409,9 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
     const uint32_t c = me + k * F::kGroup;
     if (c >= chunks) continue;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      a_st<af32x4>(out + c * 8 + 4 * h, af32x4{dw[k][4 * h], dw[k][4 * h + 1], dw[k][4 * h + 2], dw[k][4 * h + 3]});
-      a_st<af32x4>(out + chunks * 8 + c * 8 + 4 * h, af32x4{db[k][4 * h], db[k][4 * h + 1], db[k][4 * h + 2], db[k][4 * h + 3]});
+    for (int h = 0; h < (int)N / 4; ++h) {
+      a_st<af32x4>(out + c * N + 4 * h, af32x4{dw[k][4 * h], dw[k][4 * h + 1], dw[k][4 * h + 2], dw[k][4 * h + 3]});
+      a_st<af32x4>(out + (chunks + c) * N + 4 * h, af32x4{db[k][4 * h], db[k][4 * h + 1], db[k][4 * h + 2], db[k][4 * h + 3]});
     }
   }
 }
@@ -414,8 +428,8 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_grad_wide(NormGrad in) {
     float x[8], q[8], w[8], s = 0.0f, sn = 0.0f;
     for (uint64_t c = threadIdx.x; c < chunks; c += kWideThreads) {
       load8<T>(dy, c * 8, in.cols, q);  // zero behind the row's end
-      ckpt_load8(in.x, r * chunks + c, x);
-      weight8(in.weight, in.bf16, c * 8, in.cols, 1.0f, w);
+      ckpt_load(in.x, r * chunks + c, x);
+      weights_at(in.weight, in.bf16, c * 8, in.cols, 1.0f, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         q[i] *= w[i];
@@ -428,8 +442,8 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_grad_wide(NormGrad in) {
     sn *= inv;
     for (uint64_t c = threadIdx.x; c < chunks; c += kWideThreads) {
       load8<T>(dy, c * 8, in.cols, q);
-      ckpt_load8(in.x, r * chunks + c, x);
-      weight8(in.weight, in.bf16, c * 8, in.cols, 1.0f, w);
+      ckpt_load(in.x, r * chunks + c, x);
+      weights_at(in.weight, in.bf16, c * 8, in.cols, 1.0f, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) q[i] = k * (fmaf(q[i], w[i], -s) - (x[i] - m) * k * sn);
       store8<T>(static_cast<uint8_t *>(in.dx.data) + r * in.dx.ld * kEntry<T>, c * 8, in.cols, q);
@@ -447,7 +461,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_columns(NormGrad in, uint64_t
   for (uint64_t r = first; r < end; ++r) {
     float g[8], x[8];
     load8<T>(static_cast<const uint8_t *>(in.dy.data) + r * in.dy.ld * kEntry<T>, c * 8, in.cols, g);
-    ckpt_load8(in.x, r * chunks + c, x);
+    ckpt_load(in.x, r * chunks + c, x);
     const float m = in.mean[r], k = in.rstd[r];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -497,66 +511,66 @@ constexpr uint32_t kRowBlocks = 512;  // blocks that longer rows are dealt to
 uint32_t row_blocks(uint64_t rows) { return (uint32_t)(rows < kRowBlocks ? rows : kRowBlocks); }
 
 // How rows are kept: threads to a row and chunks to a thread (group 0: the row is too long).  Measured, forward and backward:
-// 16384 x 2056 in bf16 takes 89 us by groups of 128, 116 by 256; 4096 x 16384 169 us by groups of 512 that load ahead, 185 by 1,024 that
+// (through the caches) 16384 x 2056 in bf16 takes 89 us by groups of 128, 116 by 256; 4096 x 16384 169 us by groups of 512 that load ahead, 185 by 1,024 that
 // have no registers for it; 200000 x 128 59 us by groups of 16, 150 by 64.  Few rows are shared by more threads: the two kernels take 6
 // and 11 us for 1024 x 2048 by groups of 64, 6 and 7 by 256 (256 rows: 5 and 10, 4 and 4; 3000: 10 and 15, 11 and 12; 6000: 14 and 18, 17
-// and 19), for 2000 x 1024 5 and 7 by 64, 7 and 8 by 256.
+// and 19), for 2000 x 1024 5 and 7 by 64, 7 and 8 by 256.  Rows of 1,025 to 2,048 entries: bf16 8192 x 2048 42 us by 64, 43 by 128 (8192 x
+// 2047 48 and 57); fp32, whose next row takes twice the registers, 72 by 64 (the backward pass then spills), 63 by 128.
 struct Kept {
   uint32_t group, keep;
 };
-Kept kept(uint64_t rows, uint64_t cols) {
+Kept kept(uint64_t rows, uint64_t cols, bool f32) {
   const uint64_t chunks = ckpt_pitch(cols) / 8;
   const uint64_t few = chunks <= 128 ? 1024 : 4096;
-  uint32_t group = chunks <= 16 ? 16 : chunks <= 32 ? 32 : chunks <= 64 ? 64 : chunks <= 256 ? (rows < few ? 256 : 64) : chunks <= 384 && rows >= 2048 ? 128 : chunks <= 1024 ? 256 : 512;
-  uint32_t keep = group == 128 ? 3 : 1;
+  uint32_t group = chunks <= 16 ? 16 : chunks <= 32 ? 32 : chunks <= 64 ? 64 : chunks <= 256 ? (rows < few ? 256 : f32 && chunks > 128 ? 128 : 64) : chunks <= 384 && rows >= 2048 ? 128 : chunks <= 1024 ? 256 : 512;
+  uint32_t keep = group == 128 && chunks > 256 ? 3 : 1;
   while (keep < 4 && (uint64_t)group * keep < chunks) keep += group == 64 && keep == 2 ? 2 : 1;
   if ((uint64_t)group * keep < chunks) group = 0;
   return {group, keep};
 }
 // Parts of the sums over rows: blocks of the backward pass (Fit::kGroups rows at a time), or slices of the rows.
 uint32_t norm_parts(uint64_t rows, uint64_t cols) {
-  const Kept k = kept(rows, cols);
+  const Kept k = kept(rows, cols, false);  // (either way: for fp32 it differs where there are more rows than 256 blocks take at once)
   const uint64_t at_once = k.group == 0 ? 8 : k.group < 512 ? 512 / k.group : 1, parts = (rows + at_once - 1) / at_once;
   return (uint32_t)(parts < 256 ? parts : 256);
 }
-template <typename T, typename F>
+template <typename F>
 hipError_t run_norm(const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
   constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
-  const uint64_t blocks = (in.rows + kGroups - 1) / kGroups, most = 256 * (kBlock > 256 ? 1 : F::kGroup == 256 && F::kKeep > 2 ? 6 - F::kKeep : F::kGroup == 128 ? 3 : 4);
-  hipLaunchKernelGGL((k_norm<T, F>), dim3((uint32_t)(blocks < most ? blocks : most)), dim3(kBlock), 0, s, in, y, saved, mean, rstd);
+  const uint64_t blocks = (in.rows + kGroups - 1) / kGroups, most = 256 * (kBlock > 256 ? 1 : F::kGroup == 256 && F::kEights > 2 ? 6 - F::kEights : F::kGroup == 128 ? 3 : 4);
+  hipLaunchKernelGGL((k_norm<F>), dim3((uint32_t)(blocks < most ? blocks : most)), dim3(kBlock), 0, s, in, y, saved, mean, rstd);
   return hipGetLastError();
 }
-template <typename T, typename F>
+template <typename F>
 hipError_t run_norm_grad(const NormGrad &in, float *part, uint32_t parts, hipStream_t s) {
-  hipLaunchKernelGGL((k_norm_grad<T, F>), dim3(parts), dim3(F::kBlock), 0, s, in, part);
+  hipLaunchKernelGGL((k_norm_grad<F>), dim3(parts), dim3(F::kBlock), 0, s, in, part);
   return hipGetLastError();
 }
-#define DQ_FITS(run, ...)                                       \
-  switch (k.group * 8 + k.keep) {                               \
-    case 16 * 8 + 1: return run<T, Fit<16, 1>>(__VA_ARGS__);    \
-    case 32 * 8 + 1: return run<T, Fit<32, 1>>(__VA_ARGS__);    \
-    case 64 * 8 + 1: return run<T, Fit<64, 1>>(__VA_ARGS__);    \
-    case 64 * 8 + 2: return run<T, Fit<64, 2>>(__VA_ARGS__);    \
-    case 64 * 8 + 4: return run<T, Fit<64, 4>>(__VA_ARGS__);    \
-    case 128 * 8 + 3: return run<T, Fit<128, 3>>(__VA_ARGS__);  \
-    case 256 * 8 + 1: return run<T, Fit<256, 1>>(__VA_ARGS__);  \
-    case 256 * 8 + 2: return run<T, Fit<256, 2>>(__VA_ARGS__);  \
-    case 256 * 8 + 3: return run<T, Fit<256, 3>>(__VA_ARGS__);  \
-    case 256 * 8 + 4: return run<T, Fit<256, 4>>(__VA_ARGS__);  \
-    case 512 * 8 + 3: return run<T, Fit<512, 3>>(__VA_ARGS__);  \
-    case 512 * 8 + 4: return run<T, Fit<512, 4>>(__VA_ARGS__);  \
+#define DQ_FIT(run, group, keep, ...) \
+  case group * 8 + keep: return past ? run<Fit<T, group, keep, true>>(__VA_ARGS__) : run<Fit<T, group, keep, false>>(__VA_ARGS__);
+#define DQ_FITS(run, ...)                                                                                             \
+  switch (k.group * 8 + k.keep) {                                                                                     \
+    DQ_FIT(run, 16, 1, __VA_ARGS__) DQ_FIT(run, 32, 1, __VA_ARGS__)                                                   \
+    DQ_FIT(run, 64, 1, __VA_ARGS__) DQ_FIT(run, 64, 2, __VA_ARGS__) DQ_FIT(run, 64, 4, __VA_ARGS__)                   \
+    case 128 * 8 + 2:                                                                                                 \
+      if constexpr (__is_same(T, F32)) return past ? run<Fit<T, 128, 2, true>>(__VA_ARGS__) : run<Fit<T, 128, 2, false>>(__VA_ARGS__); \
+      break;                                                                                                          \
+    case 256 * 8 + 1: return run<Fit<T, 256, 1, false>>(__VA_ARGS__); /* few rows: never large */                     \
+    DQ_FIT(run, 128, 3, __VA_ARGS__)                                                                                  \
+    DQ_FIT(run, 256, 2, __VA_ARGS__) DQ_FIT(run, 256, 3, __VA_ARGS__) DQ_FIT(run, 256, 4, __VA_ARGS__) \
+    DQ_FIT(run, 512, 3, __VA_ARGS__) DQ_FIT(run, 512, 4, __VA_ARGS__)                                                 \
   }
 template <typename T>
-hipError_t norm_forward(const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
-  const Kept k = kept(in.rows, in.cols);
+hipError_t norm_forward(bool past, const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
+  const Kept k = kept(in.rows, in.cols, __is_same(T, F32));
   DQ_FITS(run_norm, in, y, saved, mean, rstd, s)
   hipLaunchKernelGGL((k_norm_wide<T>), dim3(row_blocks(in.rows)), dim3(kWideThreads), 0, s, in, y, saved, mean, rstd);
   return hipGetLastError();
 }
 // part: null if nobody wants the sums over rows.
 template <typename T>
-hipError_t norm_backward(const NormGrad &in, float *part, uint32_t parts, hipStream_t s) {
-  const Kept k = kept(in.rows, in.cols);
+hipError_t norm_backward(bool past, const NormGrad &in, float *part, uint32_t parts, hipStream_t s) {
+  const Kept k = kept(in.rows, in.cols, __is_same(T, F32));
   DQ_FITS(run_norm_grad, in, part, parts, s)
   hipLaunchKernelGGL((k_norm_grad_wide<T>), dim3(row_blocks(in.rows)), dim3(kWideThreads), 0, s, in);
   const hipError_t e = hipGetLastError();
@@ -566,6 +580,9 @@ hipError_t norm_backward(const NormGrad &in, float *part, uint32_t parts, hipStr
   return hipGetLastError();
 }
 
+bool goes_past(const dq_matrix *a, const dq_matrix *b, uint64_t rows, uint64_t cols, uint64_t least) {
+  return on_16(a, rows) && on_16(b, rows) && 2 * rows * cols * entry_bytes(a->dtype) >= least;
+}
 uint32_t join_grid(uint64_t pitch) { return (uint32_t)(2 * pitch / kJoinCols < 4096 ? 2 * pitch / kJoinCols : 4096); }
 
 bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -602,7 +619,8 @@ dq_status dq_layer_norm(const dq_matrix *x, uint64_t rows, uint64_t cols, const 
   const Rows out = {y->data, y->ld};
   const CkptOut saved = ckpt_out(ckpt, rows, cols);
   hipStream_t s = (hipStream_t)hip_stream;
-  return hip_status(x->dtype == DQ_F32 ? norm_forward<F32>(in, out, saved, mean, rstd, s) : norm_forward<Bf16>(in, out, saved, mean, rstd, s));
+  const bool past = goes_past(x, y, rows, cols, 2 * kPastBytes);
+  return hip_status(x->dtype == DQ_F32 ? norm_forward<F32>(past, in, out, saved, mean, rstd, s) : norm_forward<Bf16>(past, in, out, saved, mean, rstd, s));
 }
 
 size_t dq_layer_norm_grad_scratch_bytes(uint64_t rows, uint64_t cols) {
@@ -640,7 +658,8 @@ dq_status dq_layer_norm_grad(const dq_matrix *dy, const void *ckpt, const float 
     if (regions_meet(r, 9)) return DQ_EINVAL;
     const NormGrad in = {{dy->data, dy->ld}, {dx->data, dx->ld}, rows, cols, ckpt_in(ckpt, rows, cols), mean, rstd, weight, (uint32_t)(weight_dtype == DQ_BF16)};
     float *part = dweight ? static_cast<float *>(scratch) : nullptr;
-    DQ_TRY(hip_status(dy->dtype == DQ_F32 ? norm_backward<F32>(in, part, parts, s) : norm_backward<Bf16>(in, part, parts, s)));
+    const bool past = goes_past(dy, dx, rows, cols, kPastBytes);
+    DQ_TRY(hip_status(dy->dtype == DQ_F32 ? norm_backward<F32>(past, in, part, parts, s) : norm_backward<Bf16>(past, in, part, parts, s)));
     if (!dweight) return DQ_OK;
   }
   if (weight_dtype == DQ_F32)

@@ -139,3 +139,37 @@ def test_large_calls_give_what_calls_over_parts_give(dev, dtype, cols, ld):
         wz, wu = B.dq_gate_grad(want, kept)
         assert torch.equal(want, h[a]) and torch.equal(wz, dz[a]) and torch.equal(wu, du[a])
         assert torch.equal(B.dq_gate(z[a], None, "silu"), B.dq_gate(z, None, "silu")[a]) if k == 0 else True
+
+
+@pytest.mark.parametrize("dtype,weights", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("cols,ld", [(128, 128), (97, 128), (250, 256), (500, 504), (1000, 1000), (1029, 1032), (2048, 2048), (3000, 3000), (4096, 4096),
+                                     (5000, 5008), (6151, 6152), (9001, 9008), (12300, 12304), (16384, 16384)])
+def test_large_layer_norms(dev, dtype, weights, cols, ld):
+    """x of 128 MiB and more, in every way that rows are kept."""
+    rows = (1 << 27) // (cols * dtype.itemsize) + 5
+    whole = fill(rows, ld, dev, 5).to(dtype)
+    x = whole[:, :cols]
+    weight, bias = torch.linspace(0.5, 1.5, cols, device=dev).to(weights), torch.linspace(-1, 1, cols, device=dev).to(weights)
+    out = torch.full((rows, ld), 7.0, dtype=dtype, device=dev)
+    y, saved = B.dq_layer_norm(x, weight, bias, save=True, out=out[:, :cols])
+    some = torch.cat([torch.arange(0, rows, rows // 37, device=dev), torch.arange(rows - 3, rows, device=dev)]).unique()
+    want, mean, rstd = P.layer_norm(x[some], weight, bias, 1e-5)
+    bound, dk, dm = P.layer_norm_bound(x[some], weight, bias, 1e-5, dtype)
+    assert bool(((y[some].double() - want).abs() <= bound).all())
+    assert bool(((saved.mean[some].double() - mean.reshape(-1)).abs() <= dm.reshape(-1)).all())
+    assert bool(((saved.rstd[some].double() - rstd.reshape(-1)).abs() <= (rstd * dk).reshape(-1)).all())
+    assert torch.equal(saved.x.data, B.dq_ckpt_save(x).data)
+    del y
+    dy = torch.zeros_like(whole)[:, :cols]         # all but a few rows count nothing in the sums over rows
+    dy[some] = x[some].flip(1)
+    dx, dw, db = B.dq_layer_norm_grad(dy, saved, weight, out=out[:, :cols])
+    xv = P.held(x[some])
+    wants = P.layer_norm_grad(dy[some], xv, saved.mean[some], saved.rstd[some], weight)
+    bounds = P.layer_norm_grad_bounds(dy[some], xv, saved.mean[some], saved.rstd[some], weight, dtype, weights)
+    assert bool(((dx[some].double() - wants[0]).abs() <= bounds[0]).all())
+    rest = torch.ones(rows, dtype=torch.bool, device=dev)
+    rest[some] = False
+    assert bool((dx[rest] == 0).all()) and (ld == cols or bool((out[:, cols:] == 7.0).all()))
+    # a thread adds its rows of zeros to what it has: exact; the parts of 256 blocks are then at most 256 additions more
+    for got, v, tol in ((dw, wants[1], bounds[1]), (db, wants[2], bounds[2])):
+        assert bool(((got.double() - v).abs() <= tol * (1 + 256 / 4)).all())
