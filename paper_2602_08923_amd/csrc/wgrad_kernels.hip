@@ -66,17 +66,18 @@ __device__ __forceinline__ void put(void *out, uint64_t at, float v, uint32_t ac
     a_st<uint16_t>(p, (uint16_t)to_bf16x2(v, v));
   }
 }
-// Eight sums of row o from column i on; cols: the row's length.
+// 16 bytes of sums, at `row` from column i on; cols: the row's length.
 template <typename O>
-__device__ __forceinline__ void put8(const WGrad &g, uint64_t o, uint64_t i, float (&v)[8]) {
-  uint8_t *row = static_cast<uint8_t *>(g.dw) + o * g.ld * kEntry<O>;
-  if (g.accumulate) {
-    float old[8];
-    load8<O>(row, i, g.cols, old);
+constexpr uint32_t kPut = 16 / kEntry<O>;
+template <typename O>
+__device__ __forceinline__ void put16(void *row, uint64_t i, uint64_t cols, uint32_t accumulate, float (&v)[kPut<O>]) {
+  if (accumulate) {
+    float old[kPut<O>];
+    load_entries<O, kPut<O>>(row, i, cols, old);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += old[k];
+    for (uint32_t k = 0; k < kPut<O>; ++k) v[k] += old[k];
   }
-  store8<O>(row, i, g.cols, v);
+  store_entries<O, kPut<O>>(row, i, cols, v);
 }
 
 // A block's tile: kOut x kIn sums, kTok tokens a step; its waves, 2 by WAVES_IN, have kWaveOut x kWaveIn each.
@@ -107,14 +108,17 @@ __device__ __forceinline__ uint64_t tile_in(const WGrad &g, uint64_t tile) {
   const uint64_t s = tile_strip(g, tile);
   return s + (tile - s * g.tiles_out) % strip_width(g, s);
 }
-// Which of dy's columns column c of a tile holds (see begin()); outs or more: none, or one that another column holds too.
+// Which of a tile's columns of dy, of which `outs` exist, its column c holds (see begin()); outs or more: none, or one that another
+// column holds too.
 template <bool SMALL>
-__device__ __forceinline__ uint64_t column(uint64_t outs, uint64_t o0, uint32_t c) {
-  const uint64_t chunk = o0 + (c & ~7u);
-  if (SMALL || chunk >= outs || chunk + 8 <= outs) return o0 + c;
-  const uint32_t shift = (uint32_t)(chunk + 8 - outs);
-  return (c & 7u) < shift ? outs : o0 + c - shift;
+__device__ __forceinline__ uint32_t column(uint32_t outs, uint32_t c) {
+  const uint32_t chunk = c & ~7u;
+  if (SMALL || chunk >= outs || chunk + 8 <= outs) return c;
+  const uint32_t shift = chunk + 8 - outs;
+  return (c & 7u) < shift ? outs : c - shift;
 }
+template <typename S>
+__device__ __forceinline__ uint32_t tile_outs(const WGrad &g, uint64_t o0) { return g.outs - o0 < S::kOut ? (uint32_t)(g.outs - o0) : S::kOut; }
 // What a lane has on its way from memory: its part of a step.
 template <typename T, typename S>
 struct Stage {
@@ -356,17 +360,18 @@ struct Walker {
     for (; step + 2 < last; ++step) advance<BIAS, true>(step, last);
     for (; step <= last; ++step) advance<BIAS, false>(step, last);
   }
-  // A product's 32 x 32 sums go through a patch of LDS of the wave's own, so that a lane has 16 of a row.
+  // A product's 32 x 32 sums go through a patch of LDS of the wave's own, so that the lanes of a row have 16 bytes each, side by side
+  // (with half a row to a lane, stores covered lines in parts: one token, 8192 x 8192, fp32 54 us and 91, bf16 40 and 44).
   __device__ __forceinline__ void put_tile() {
-    constexpr uint32_t kRow = 144;
+    constexpr uint32_t kRow = 144, kLanes = 32 / kPut<O>, kRows = 64 / kLanes;  // lanes to a row, rows at once
     uint32_t l = threadIdx.x & 63u;
     asm volatile("" : "+v"(l));  // what follows from it is worked out here, not kept in registers through the steps
-    const uint32_t patch = base + wave * (32 * kRow), to = patch + 4 * (l >> 5) * kRow + (l & 31u) * 4, from = patch + (l >> 1) * kRow + (l & 1u) * 64;
-    const uint32_t c = (wave & 1u) * S::kWaveOut + (l >> 1);
-    const uint64_t i = i0 + (wave >> 1) * S::kWaveIn + (l & 1u) * 16;
+    const uint32_t patch = base + wave * (32 * kRow), to = patch + 4 * (l >> 5) * kRow + (l & 31u) * 4, from = patch + l / kLanes * kRow + l % kLanes * (kPut<O> * 4);
+    const uint32_t c = (wave & 1u) * S::kWaveOut + l / kLanes, outs = tile_outs<S>(g, o0);
+    const uint64_t i = i0 + (wave >> 1) * S::kWaveIn + l % kLanes * kPut<O>, row_bytes = g.ld * kEntry<O>;
+    uint8_t *const dw = static_cast<uint8_t *>(g.dw) + o0 * row_bytes;
 #pragma unroll
-    for (uint32_t m = 0; m < S::kM; ++m) {
-      const uint64_t o = column<SMALL>(g.outs, o0, c + m * 32);
+    for (uint32_t m = 0; m < S::kM; ++m)
 #pragma unroll
       for (uint32_t n = 0; n < S::kN; ++n) {
         __builtin_amdgcn_sched_barrier(0);
@@ -375,21 +380,26 @@ struct Walker {
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        float v[2][8];
+        float v[32 / kRows][kPut<O>];
 #pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-          const a32x4 w = *reinterpret_cast<lds_a32x4 *>(from + q * 16);
+        for (uint32_t h = 0; h < 32 / kRows; ++h)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[q / 2][q % 2 * 4 + k] = a_float(w[k]);
-        }
+          for (uint32_t q = 0; q < kPut<O> / 4; ++q) {
+            const a32x4 w = *reinterpret_cast<lds_a32x4 *>(from + h * kRows * kRow + q * 16);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[h][q * 4 + k] = a_float(w[k]);
+          }
         __builtin_amdgcn_wave_barrier();
-        if (o < g.outs) {
+        if (i + n * 32 < g.cols) {
+          uint32_t first_row = c + m * 32;
+          asm volatile("" : "+v"(first_row));  // (nor these rows' addresses for all products)
 #pragma unroll
-          for (uint32_t h = 0; h < 2; ++h)
-            if (i + n * 32 + h * 8 < g.cols) put8<O>(g, o, i + n * 32 + h * 8, v[h]);
+          for (uint32_t h = 0; h < 32 / kRows; ++h) {
+            const uint32_t o = column<SMALL>(outs, first_row + h * kRows);
+            if (o < outs) put16<O>(dw + o * row_bytes, i + n * 32, g.cols, g.accumulate, v[h]);
+          }
         }
       }
-    }
   }
   __device__ __forceinline__ void put_part(uint64_t unit) {
     const uint64_t o = o0 + (wave & 1u) * S::kWaveOut, i = i0 + (wave >> 1) * S::kWaveIn;
@@ -410,19 +420,20 @@ struct Walker {
 #pragma unroll
     for (int i = 0; i < 8; ++i) *reinterpret_cast<lds_float *>(to + 4 * i) = sums[i];
     lds_barrier();
+    const uint32_t outs = tile_outs<S>(g, o0);
     for (uint32_t c = threadIdx.x; c < S::kOut; c += S::kThreads) {
       float v = 0.0f;
       for (uint32_t r = 0; r < S::kOutRows; ++r) v += *reinterpret_cast<lds_float *>(base + (r * S::kOut + c) * 4);
-      const uint64_t o = column<SMALL>(g.outs, o0, c);
-      if (o >= g.outs) continue;
-      if (g.splits > 1) a_st<float>(g.part + units * (S::kOut * S::kIn) + split * g.outs + o, v);
-      else put<O>(g.db, o, v, g.accumulate);
+      const uint32_t o = column<SMALL>(outs, c);
+      if (o >= outs) continue;
+      if (g.splits > 1) a_st<float>(g.part + units * (S::kOut * S::kIn) + split * g.outs + o0 + o, v);
+      else put<O>(g.db, o0 + o, v, g.accumulate);
     }
   }
 };
 
 template <typename T, typename O, typename S, bool SMALL>
-__global__ __launch_bounds__(S::kThreads) void k_wgrad(WGrad g) {
+__global__ __launch_bounds__(S::kThreads, S::kOut > 64 ? 2 : 3) void k_wgrad(WGrad g) {  // waves to a SIMD, as many as LDS lets in
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * S::kBuffer];
   Walker<T, O, S, SMALL> w(g, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds);
   const uint64_t units = g.tiles * g.splits;
@@ -489,8 +500,8 @@ __global__ __launch_bounds__(kJoinThreads) void k_wgrad_join(WGrad g) {
     if (i < quads) {
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) {
-        const uint64_t o = column<SMALL>(g.outs, o0, row + r);
-        if (o < g.outs) put<O>(g.dw, o * g.ld + at, v[r], g.accumulate);
+        const uint32_t outs = tile_outs<S>(g, o0), o = column<SMALL>(outs, row + r);
+        if (o < outs) put<O>(g.dw, (o0 + o) * g.ld + at, v[r], g.accumulate);
       }
     } else {
       put<O>(g.db, i - quads, v[0], g.accumulate);
