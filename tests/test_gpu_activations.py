@@ -472,7 +472,7 @@ def test_gradients_against_differences(dev):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,cols", [(1, 100), (33, 128), (5000, 129), (70, 256), (9, 200), (40000, 17), (20001, 250), (9000, 500), (2500, 3000), (600, 4099), (2200, 5000), (700, 12300), (600, 16384), (300, 8193)])
+@pytest.mark.parametrize("rows,cols", [(1, 100), (33, 128), (5000, 129), (70, 256), (9, 200), (40000, 17), (20001, 250), (9000, 500), (4100, 1500), (5000, 2048), (4097, 1025), (2500, 3000), (600, 4099), (2200, 5000), (700, 12300), (600, 16384), (300, 8193)])
 def test_layer_norm_of_every_way_to_keep_rows(dev, rows, cols, dtype):
     """Short rows that share a wave, and blocks that take several rows."""
     t = TYPES[dtype]
