@@ -17,7 +17,6 @@ typedef float af32x4 __attribute__((ext_vector_type(4)));
 typedef float af32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef a32x4 a32x4_any __attribute__((aligned(2)));   // 16 bytes from any bf16's address
-typedef af32x4 af32x4_any __attribute__((aligned(4)));
 
 // rows x cols entries, row r from data + r * ld entries on
 struct Rows {

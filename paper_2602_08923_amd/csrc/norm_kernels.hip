@@ -522,7 +522,10 @@ struct Kept {
 Kept kept(uint64_t rows, uint64_t cols, bool f32) {
   const uint64_t chunks = ckpt_pitch(cols) / 8;
   const uint64_t few = chunks <= 128 ? 1024 : 4096;
-  uint32_t group = chunks <= 16 ? 16 : chunks <= 32 ? 32 : chunks <= 64 ? 64 : chunks <= 256 ? (rows < few ? 256 : f32 && chunks > 128 ? 128 : 64) : chunks <= 384 && rows >= 2048 ? 128 : chunks <= 1024 ? 256 : 512;
+  uint32_t group = 512;
+  if (chunks <= 64) group = chunks <= 16 ? 16 : chunks <= 32 ? 32 : 64;
+  else if (chunks <= 256) group = rows < few ? 256 : f32 && chunks > 128 ? 128 : 64;
+  else if (chunks <= 1024) group = chunks <= 384 && rows >= 2048 ? 128 : 256;
   uint32_t keep = group == 128 && chunks > 256 ? 3 : 1;
   while (keep < 4 && (uint64_t)group * keep < chunks) keep += group == 64 && keep == 2 ? 2 : 1;
   if ((uint64_t)group * keep < chunks) group = 0;
@@ -530,7 +533,7 @@ Kept kept(uint64_t rows, uint64_t cols, bool f32) {
 }
 // Parts of the sums over rows: blocks of the backward pass (Fit::kGroups rows at a time), or slices of the rows.
 uint32_t norm_parts(uint64_t rows, uint64_t cols) {
-  const Kept k = kept(rows, cols, false);  // (either way: for fp32 it differs where there are more rows than 256 blocks take at once)
+  const Kept k = kept(rows, cols, false);  // (fp32 differs only where there are rows enough for 256 parts either way)
   const uint64_t at_once = k.group == 0 ? 8 : k.group < 512 ? 512 / k.group : 1, parts = (rows + at_once - 1) / at_once;
   return (uint32_t)(parts < 256 ? parts : 256);
 }
