@@ -85,10 +85,20 @@ __global__ __launch_bounds__(kMapThreads) void k_ckpt_load(Walk8 w, CkptIn in, R
 
 // a = act(z), d = act'(z).  The exponential and the reciprocal are the hardware's: over whole octaves they were off by 1.42 and 1.53 half
 // steps at most, 0.45 and 0.48 in the mean square; what would be a subnormal number they make zero.
-template <int KIND>
+template <typename T, int KIND>
 __device__ __forceinline__ void activation(float z, float *a, float *d) {
   if constexpr (KIND == DQ_SILU) {  // z p with p = 1 / (1 + e^-z); the derivative is p + z p (1 - p)
-    const float p = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+    float p;
+    if constexpr (__is_same(T, F32)) {
+      // -z log2 e is x + rest, x as rounded: p(x + rest) is p + p (p - 1) rest ln 2.  Without the rest e^-z would be off by |z| half steps
+      // (which a bf16 result, of 2^16 times larger steps, does not show).  Beyond +-100 p is zero or one, and rest might not be finite.
+      const float c = __builtin_amdgcn_fmed3f(z, -100.0f, 100.0f), x = c * -1.44269504f;
+      const float rest = fmaf(c, -1.92596299e-8f, fmaf(c, -1.44269504f, -x));
+      p = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x));
+      p = fmaf(p * (p - 1.0f), rest * 0.693147181f, p);
+    } else {
+      p = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+    }
     *a = z * p;
     *d = p * fmaf(z, 1.0f - p, 1.0f);
   } else {
@@ -125,7 +135,7 @@ __global__ __launch_bounds__(kMapThreads) void k_gate(Walk8 w, Rows z, Rows u, R
 #pragma unroll
     for (uint32_t k = 0; k < kChunk<T>; ++k) {
       float d;
-      activation<KIND>(a.v[k], &a.v[k], &d);
+      activation<T, KIND>(a.v[k], &a.v[k], &d);
       if constexpr (GATED) a.v[k] *= b.v[k];
     }
     store_entries<T, kChunk<T>, PAST>(row_of<T>(h, i.row), i.at * kChunk<T>, w.cols, a.v);
@@ -140,7 +150,7 @@ __global__ __launch_bounds__(kMapThreads) void k_gate_grad(Walk8 w, Rows dh, Ckp
 #pragma unroll
     for (uint32_t k = 0; k < kChunk<T>; ++k) {
       float act, d;
-      activation<KIND>(a.v[k], &act, &d);
+      activation<T, KIND>(a.v[k], &act, &d);
       if constexpr (GATED) {
         a.v[k] = g.v[k] * b.v[k] * d;
         b.v[k] = g.v[k] * act;
