@@ -13,11 +13,20 @@ namespace {
 constexpr uint32_t kWideThreads = 1024, kThreads = 256;
 
 // The sum over a wave, or over each 16 or 32 of its lanes, in all of them: within rows of 16 lanes by moves that the addition makes
-// itself, then over the rows (a swap of two copies' rows, or halves, leaves what is to be added in the two).  Through LDS, as
-// shuffles go, a sum took 100 cycles a step.
+// itself, then over the rows and the halves.  Through LDS, as shuffles go, a sum took 100 cycles a step.
 template <int CTRL>
 __device__ __forceinline__ float add_dpp(float v) {
   return v + a_float((uint32_t)__builtin_amdgcn_mov_dpp((int)a_bits(v), CTRL, 0xF, 0xF, true));
+}
+// A swap of a's odd rows with b's even ones (of a's upper half with b's lower one) leaves two values whose sum has a's neighbouring rows (halves)
+// added up in a's places, b's in b's.
+__device__ __forceinline__ float rows_sum(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(a_bits(a), a_bits(b), false, false);
+  return a_float(r[0]) + a_float(r[1]);
+}
+__device__ __forceinline__ float halves_sum(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a_bits(a), a_bits(b), false, false);
+  return a_float(r[0]) + a_float(r[1]);
 }
 template <uint32_t LANES = 64>
 __device__ __forceinline__ float lanes_sum(float v) {
@@ -25,14 +34,8 @@ __device__ __forceinline__ float lanes_sum(float v) {
   v = add_dpp<0x4E>(v);   // lanes 2 3 0 1
   v = add_dpp<0x141>(v);  // mirrored within 8
   v = add_dpp<0x140>(v);  // mirrored within 16
-  if constexpr (LANES > 16) {
-    const auto a = __builtin_amdgcn_permlane16_swap(a_bits(v), a_bits(v), false, false);
-    v = a_float(a[0]) + a_float(a[1]);
-  }
-  if constexpr (LANES > 32) {
-    const auto b = __builtin_amdgcn_permlane32_swap(a_bits(v), a_bits(v), false, false);
-    v = a_float(b[0]) + a_float(b[1]);
-  }
+  if constexpr (LANES > 16) v = rows_sum(v, v);
+  if constexpr (LANES > 32) v = halves_sum(v, v);
   return v;
 }
 // Sums of a and b over the block, in every thread; the order is fixed.
@@ -81,8 +84,8 @@ __device__ __forceinline__ void weights_at(const void *w, uint32_t bf16, uint64_
 // PAST: rows of large calls go past the caches.  A wave's loads and stores then have to cover memory without gaps, so a chunk is 16 bytes,
 // twice as many of 4 entries in fp32.  Forward and backward, through the caches and past them: bf16 65536 x 2048 265 and 228 us,
 // 16384 x 4096 136 and 128, fp32 16384 x 4096 231 and 207.  Below, chunks of 8 are as good or better (fp32 1024 x 8192 41 and 43), and
-// better over odd rows (fp32 3000 x 7001 96, 105 with 4).  The forward pass takes twice the size for large (bf16 16384 x 2048 by itself
-// 21.9 and 24.3 us: the matrix that it reads may still be in the caches).
+// better over odd rows (fp32 3000 x 7001 96, 105 with 4).  Both add a row up in the same order (see RowSums).  The forward pass takes twice
+// the size for large (bf16 16384 x 2048 by itself 21.9 and 24.3 us: the matrix that it reads may still be in the caches).
 //
 // A block's groups take a row each, the block then the next rows; all of them come round as often as each other.
 template <typename T, uint32_t GROUP, uint32_t KEEP, bool PAST>
@@ -93,26 +96,78 @@ struct Fit {
   static constexpr bool kPast = PAST, kAheadBackward = GROUP <= 64 || KEEP <= 3;  // with more, the backward pass has no registers to load ahead
   static constexpr uint32_t kBlock = 512, kGroups = kBlock / GROUP;  // of the backward pass
 };
-// Sums of a and b over a group, in all its threads; the order is fixed.  All threads of the block come here.
-template <uint32_t GROUP>
-__device__ __forceinline__ void group_sums(float &a, float &b, af32x2 *lds) {
-  constexpr uint32_t kLanes = GROUP < 64 ? GROUP : 64;
-  a = lanes_sum<kLanes>(a);
-  b = lanes_sum<kLanes>(b);
-  if constexpr (GROUP > 64) {
-    const uint32_t wave = threadIdx.x >> 6, first = wave / (GROUP / 64) * (GROUP / 64);
-    __syncthreads();  // the last sums have been read
-    if ((threadIdx.x & 63u) == 0) lds[wave] = af32x2{a, b};
-    __syncthreads();
-    a = b = 0.0f;
+// SUMS sums over a row, in an order that does not depend on where rows lie.  bf16: a thread's entries, one after the other; the group's
+// threads in pairs, fours and so on up to 64; the waves.  fp32, whose chunks are 8 entries or 4: of a thread's chunks of 8 the first fours, one
+// after the other, and the second ones; the two; threads and waves as above.
+//
+// Where a chunk is 4, the two fours of 8 are neighbouring lanes'.  Eight number l + GROUP k, thread l's chunk k where chunks are 8, is two lanes'
+// chunk 2 k if l is in the lower half of the group, and 2 k + 1 if not: a thread has the first, or second, fours of two threads, and
+// two waves together have those of 64.
+template <typename F, uint32_t SUMS>
+struct RowSums {
+  static constexpr bool kFours = __is_same(typename F::Type, F32), kShared = F::kEntries == 4;
+  static constexpr uint32_t kOwn = kFours ? 2 : 1, kLeft = kShared ? 2 : 1;  // a thread's sums, and those that a wave leaves
+  float v[SUMS][kOwn];
+  typedef float Slot[SUMS * kLeft];  // of LDS, one for each wave of the block
+  __device__ __forceinline__ RowSums() {
 #pragma unroll
-    for (uint32_t i = 0; i < GROUP / 64; ++i) {
-      const af32x2 v = lds[first + i];
-      a += v.x;
-      b += v.y;
+    for (uint32_t s = 0; s < SUMS; ++s)
+#pragma unroll
+      for (uint32_t h = 0; h < kOwn; ++h) v[s][h] = 0.0f;
+  }
+  // What entry i of a thread's chunk k is added to.
+  __device__ __forceinline__ float &of(uint32_t s, uint32_t k, uint32_t i) { return v[s][kShared ? k % 2 : kFours ? i / 4 : 0]; }
+  // The sums, in all threads of the group.  All threads of the block come here.
+  __device__ __forceinline__ void group(float (&out)[SUMS], Slot *lds) {
+    constexpr uint32_t kLanes = F::kGroup < 64 ? F::kGroup : 64, kWaves = F::kGroup / 64;
+    const uint32_t wave = threadIdx.x >> 6;
+    if constexpr (kShared && SUMS == 2 && kWaves > 1) {
+      // four sums: within rows of 16 lanes each, then a swap of rows adds up two of them at once, one of halves all four, which leaves a row each
+      float w[4];
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) w[i] = lanes_sum<16>(v[i / 2][i % 2]);
+      const float all = halves_sum(rows_sum(w[0], w[1]), rows_sum(w[2], w[3]));
+      __syncthreads();  // the last sums have been read
+      if ((threadIdx.x & 15u) == 0) lds[wave][(threadIdx.x & 63u) >> 4] = all;
+    } else {
+      float w[SUMS][kLeft];
+#pragma unroll
+      for (uint32_t s = 0; s < SUMS; ++s) {
+        if constexpr (kShared) {
+          w[s][0] = lanes_sum<kLanes>(v[s][0]);
+          w[s][1] = lanes_sum<kLanes>(v[s][1]);
+        } else {
+          w[s][0] = lanes_sum<kLanes>(kFours ? v[s][0] + v[s][kOwn - 1] : v[s][0]);
+        }
+      }
+      if constexpr (kWaves <= 1) {
+#pragma unroll
+        for (uint32_t s = 0; s < SUMS; ++s) out[s] = kShared ? w[s][0] + w[s][kLeft - 1] : w[s][0];
+      } else {
+        __syncthreads();  // the last sums have been read
+        if ((threadIdx.x & 63u) == 0) {
+#pragma unroll
+          for (uint32_t s = 0; s < SUMS; ++s)
+#pragma unroll
+            for (uint32_t h = 0; h < kLeft; ++h) lds[wave][s * kLeft + h] = w[s][h];
+        }
+      }
+    }
+    if constexpr (kWaves > 1) {
+      const uint32_t first = wave / kWaves * kWaves;
+      __syncthreads();
+#pragma unroll
+      for (uint32_t s = 0; s < SUMS; ++s) {
+        out[s] = 0.0f;
+#pragma unroll
+        for (uint32_t h = 0; h < kLeft; ++h)
+#pragma unroll
+          for (uint32_t i = 0; i < kWaves; i += kLeft)
+            out[s] += kShared ? lds[first + i][s * kLeft + h] + lds[first + i + kLeft - 1][s * kLeft + h] : lds[first + i][s];
+      }
     }
   }
-}
+};
 
 // A weight (or a bias) as the threads of a group read it, a chunk at a time: from registers, or, where a wave has a row and many
 // rows pass, from LDS, which leaves registers for the next row.
@@ -155,8 +210,9 @@ struct Weight {
 template <typename F>
 __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(NormIn in, Rows y, CkptOut saved, float *mean, float *rstd) {
   typedef typename F::Type T;
+  typedef RowSums<F, 1> Sum;
   constexpr uint32_t N = F::kEntries, kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;
-  __shared__ af32x2 lds[kBlock / 64];
+  __shared__ __attribute__((aligned(16))) typename Sum::Slot lds[kBlock / 64];
   __shared__ __attribute__((aligned(16))) float weights[2][Weight<F>::kLds];
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / N), me = threadIdx.x % F::kGroup, cols = (uint32_t)in.cols;
   const float inv = 1.0f / (float)in.cols;
@@ -177,17 +233,18 @@ __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(Norm
   load(r);
   for (uint64_t first = (uint64_t)blockIdx.x * kGroups; first < in.rows; first += step, r += step) {
     const bool here = r < in.rows;
-    float v[F::kKeep][N], s = 0.0f, none = 0.0f;
+    float v[F::kKeep][N], s[1];
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) widen(next[k], v[k]);
     load(r + step);
+    Sum sum;
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k)
 #pragma unroll
-      for (int i = 0; i < (int)N; ++i) s += v[k][i];
-    group_sums<F::kGroup>(s, none, lds);
-    const float m = s * inv;
-    s = none = 0.0f;
+      for (int i = 0; i < (int)N; ++i) sum.of(0, k, i) += v[k][i];
+    sum.group(s, lds);
+    const float m = s[0] * inv;
+    Sum squares;
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
       int left = (int)cols - (int)((me + k * F::kGroup) * N);  // of the row from this chunk on
@@ -196,19 +253,19 @@ __global__ __launch_bounds__(F::kGroup < 256 ? 256 : F::kGroup) void k_norm(Norm
 #pragma unroll
         for (int i = 0; i < (int)N; ++i) {
           const float d = v[k][i] - m;
-          s = fmaf(d, d, s);
+          squares.of(0, k, i) = fmaf(d, d, squares.of(0, k, i));
         }
       } else if (left > 0) {
 #pragma unroll
         for (int i = 0; i < (int)N; ++i) {
           const float d = i < left ? v[k][i] - m : 0.0f;
-          s = fmaf(d, d, s);
+          squares.of(0, k, i) = fmaf(d, d, squares.of(0, k, i));
         }
       }
     }
-    group_sums<F::kGroup>(s, none, lds);
+    squares.group(s, lds);
     if (!here) continue;
-    const float scale = 1.0f / sqrtf(fmaf(s, inv, in.eps));
+    const float scale = 1.0f / sqrtf(fmaf(s[0], inv, in.eps));
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
       const uint32_t c = me + k * F::kGroup;
@@ -288,9 +345,10 @@ template <typename F>
 __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *part) {
   typedef typename F::Type T;
   constexpr uint32_t N = F::kEntries;
+  typedef RowSums<F, 2> Sums;
   constexpr bool kAhead = F::kAheadBackward;
-  __shared__ af32x2 lds[F::kBlock / 64];
-  __shared__ __attribute__((aligned(16))) float weights[Weight<F>::kLds], sums[F::kGroups > 1 ? F::kGroups / 2 * F::kGroup * F::kKeep * N * 2 : 4];
+  __shared__ __attribute__((aligned(16))) typename Sums::Slot lds[F::kBlock / 64];
+  __shared__ __attribute__((aligned(16))) float weights[Weight<F>::kLds], columns[F::kGroups > 1 ? F::kGroups / 2 * F::kGroup * F::kKeep * N * 2 : 4];
   const uint32_t chunks = (uint32_t)(ckpt_pitch(in.cols) / N), me = threadIdx.x % F::kGroup, group = threadIdx.x / F::kGroup, cols = (uint32_t)in.cols;
   const float inv = 1.0f / (float)in.cols;
   const Weight<F> w(in.weight, in.bf16, cols, 1.0f, weights);
@@ -312,9 +370,11 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
       next_scale = a_ld<float>(in.rstd + r);
     }
     const uint8_t *dy = static_cast<const uint8_t *>(in.dy.data) + r * in.dy.ld * kEntry<T>;
+    uint32_t at = me;
+    if constexpr (Sums::kShared && !kAhead) asm volatile("" : "+v"(at));  // (the chunks' places are worked out here, not kept in registers between rows)
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
-      const uint32_t c = me + k * F::kGroup;
+      const uint32_t c = at + k * F::kGroup;
       next[k] = Raw<T, N>{};
       codes[k] = CkptCodes<N>{};
       scales[k] = kCkptLeast;
@@ -331,7 +391,7 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
   for (uint64_t first = (uint64_t)blockIdx.x * F::kGroups; first < in.rows; first += step, r += step) {
     const bool here = r < in.rows;
     if (!kAhead) load(r);
-    float g[F::kKeep][N], n[F::kKeep][N], s = 0.0f, sn = 0.0f;
+    float g[F::kKeep][N], n[F::kKeep][N], s[2];
     const float m = next_m, scale = next_scale;
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
@@ -339,6 +399,7 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
       ckpt_decode(codes[k], scales[k], n[k]);
     }
     if (kAhead) load(r + step);
+    Sums sums;  // of q and of q n
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
       float wk[N];
@@ -349,20 +410,20 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
         dw[k][i] = fmaf(g[k][i], n[k][i], dw[k][i]);
         db[k][i] += g[k][i];
         g[k][i] *= wk[i];
-        s += g[k][i];
-        sn = fmaf(g[k][i], n[k][i], sn);
+        sums.of(0, k, i) += g[k][i];
+        sums.of(1, k, i) = fmaf(g[k][i], n[k][i], sums.of(1, k, i));
       }
     }
-    group_sums<F::kGroup>(s, sn, lds);
+    sums.group(s, lds);
     if (!here) continue;
-    s *= inv;
-    sn *= inv;
+    s[0] *= inv;
+    s[1] *= inv;
 #pragma unroll
     for (uint32_t k = 0; k < F::kKeep; ++k) {
       const uint32_t c = me + k * F::kGroup;
       if (c >= chunks) continue;
 #pragma unroll
-      for (int i = 0; i < (int)N; ++i) g[k][i] = scale * ((g[k][i] - s) - n[k][i] * sn);
+      for (int i = 0; i < (int)N; ++i) g[k][i] = scale * ((g[k][i] - s[0]) - n[k][i] * s[1]);
       store_entries<T, N, F::kPast>(static_cast<uint8_t *>(in.dx.data) + r * in.dx.ld * kEntry<T>, c * N, cols, g[k]);
     }
   }
@@ -371,7 +432,7 @@ __global__ __launch_bounds__(F::kBlock) void k_norm_grad(NormGrad in, float *par
   // The upper half of the groups leaves its sums in LDS, the lower half adds them, until one group has them all.
   typedef __attribute__((address_space(3))) af32x4 lds_quad;
   constexpr uint32_t kSlot = F::kGroup * F::kKeep * N / 2;  // quads of a group's sums, dw's then db's, as the weights lie: 16 bytes a lane, side by side
-  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)sums + me * 16;
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)columns + me * 16;
 #pragma unroll
   for (uint32_t half = F::kGroups / 2; half; half /= 2) {
     const bool gives = group >= half && group < 2 * half, takes = group < half;
