@@ -335,11 +335,11 @@ def dq_layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, out=None):
     return y, SavedNorm(Checkpoint(data, rows, cols), mean, rstd)
 
 
-def dq_layer_norm_grad(dy, saved, weight=None, out=None, weight_out=None, bias_out=None, accumulate=False):
-    """(dx, dweight, dbias), the last two in weight's type, or None without a weight.  accumulate: added to weight_out and bias_out,
-    which then have to be given."""
+def dq_layer_norm_grad(dy, saved, weight=None, out=None, weight_out=None, bias_out=None, accumulate=False, bias=False):
+    """(dx, dweight, dbias), the last two in weight's type.  Without a weight dweight is None, and dbias too unless `bias` asks for it, or
+    bias_out is given (in bias_out's type, or dy's).  accumulate: added to weight_out and bias_out, which then have to be given."""
     x, mean, rstd = saved
-    return _native().layer_norm_grad(dy, *x, mean, rstd, weight, out, weight_out, bias_out, bool(accumulate))
+    return _native().layer_norm_grad(dy, *x, mean, rstd, weight, out, weight_out, bias_out, bool(accumulate), bool(bias))
 
 
 def dq_gate(z, u=None, kind="silu", save=False, out=None):

@@ -755,8 +755,8 @@ PyObject *py_layer_norm(PyObject *const *a, Py_ssize_t nargs) {  // x, weight, b
   if (!save) return give(a[5], out);
   return tuple({give(a[5], out), wrap(ckpt), PyLong_FromLongLong(m.rows), PyLong_FromLongLong(m.cols), wrap(mean), wrap(rstd)});
 }
-PyObject *py_layer_norm_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, data, rows, cols, mean, rstd, weight, out, weight_out, bias_out, accumulate
-  DQ_ARGS(11)
+PyObject *py_layer_norm_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, data, rows, cols, mean, rstd, weight, out, weight_out, bias_out, accumulate, bias
+  DQ_ARGS(12)
   const at::Tensor &dy = tensor(a[0]), &mean = tensor(a[4]), &rstd = tensor(a[5]), *weight = tensor_or_null(a[6]);
   const OnDevice here(dy);
   here.with(mean);
@@ -766,11 +766,11 @@ PyObject *py_layer_norm_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, dat
   const Saved x = saved_of(a + 1, here);
   if (x.rows != g.rows || x.cols != g.cols) fail("dy has another shape than the checkpoint");
   void *mu = vector_of(&mean, g.rows, at::kFloat, "mean"), *rs = vector_of(&rstd, g.rows, at::kFloat, "rstd");
-  const at::ScalarType wt = weight_type(weight, nullptr);
+  const bool accumulate = flag(a[10]), bias = weight || flag(a[11]) || a[9] != Py_None;
+  const at::ScalarType wt = bias ? weight_type(weight, weight ? nullptr : a[9] == Py_None ? &dy : &tensor(a[9])) : at::kFloat;
   void *w = vector_of(weight, g.cols, wt, "weight");
-  const bool accumulate = flag(a[10]);
-  if (!weight && (a[8] != Py_None || a[9] != Py_None || accumulate)) fail("without a weight there are no gradients of weight and bias");
-  if (accumulate && (a[8] == Py_None || a[9] == Py_None)) fail("accumulate adds to weight_out and bias_out: give them");
+  if (!weight && (a[8] != Py_None || (accumulate && !bias))) fail("without a weight there is no gradient of one");
+  if (accumulate && ((weight && a[8] == Py_None) || a[9] == Py_None)) fail("accumulate adds to weight_out and bias_out: give them");
   const at::Tensor out = a[7] == Py_None ? make_shaped(dy.sizes(), dy.scalar_type(), dy) : tensor(a[7]);
   here.with(out);
   const Act d = act_of(out, "out");
@@ -778,7 +778,7 @@ PyObject *py_layer_norm_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, dat
   at::Tensor dw, db, scratch;
   void *pw = nullptr, *pb = nullptr, *t = nullptr;
   size_t bytes = 0;
-  if (weight) {
+  if (bias) {  // (without a weight, what would be its gradient is thrown away)
     dw = a[8] == Py_None ? make_row(g.cols, wt, dy) : tensor(a[8]);
     db = a[9] == Py_None ? make_row(g.cols, wt, dy) : tensor(a[9]);
     here.with(dw);
@@ -791,8 +791,7 @@ PyObject *py_layer_norm_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, dat
   }
   void *c = ckpt_ptr(*x.data, x.rows, x.cols), *s = stream();
   CALL(dq_layer_norm_grad(&g.m, c, as<float>(mu), as<float>(rs), g.rows, g.cols, w, dtype_of(wt), &d.m, pw, pb, accumulate, t, bytes, s));
-  if (!weight) return tuple({give(a[7], out), none(), none()});
-  return tuple({give(a[7], out), give(a[8], dw), give(a[9], db)});
+  return tuple({give(a[7], out), weight ? give(a[8], dw) : none(), bias ? give(a[9], db) : none()});
 }
 PyObject *py_gate(PyObject *const *a, Py_ssize_t nargs) {  // kind, z, u, save, out
   DQ_ARGS(5)
