@@ -275,6 +275,8 @@ def dq_mx_decompress(fmt, packed_in, n_entries, local=None, out=None):
 # ---- 8-bit activation checkpoints and the passes that write and read them ---------------
 # Tensors are of any number of dimensions: the last one's entries lie side by side, the others have one distance from row to row (a
 # part of a wider tensor is such a tensor; others take a .contiguous() first).  Calls run on the current stream of their tensors' device.
+# Autograd does not record them: what they return has no graph, the gradients are the ..._grad calls'.  A tensor given for an output counts
+# as changed in place.
 
 class Checkpoint(NamedTuple):
     """rows x cols activations in 8 bits: data (uint8, 16-byte aligned) holds dq_ckpt_bytes(rows, cols) bytes (include/dq.h has their order)."""

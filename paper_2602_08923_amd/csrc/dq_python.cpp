@@ -666,6 +666,11 @@ PyObject *tuple(std::initializer_list<PyObject *> v) {
   for (PyObject *o : v) PyTuple_SET_ITEM(t, i++, o);
   return t;
 }
+// A new tensor, or the caller's own that the call wrote to: autograd, which may have kept it, is told so.
+PyObject *wrote(PyObject *given, const at::Tensor &t) {
+  if (given != Py_None && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  return give(given, t);
+}
 PyObject *none() {
   Py_INCREF(Py_None);
   return Py_None;
@@ -679,7 +684,7 @@ PyObject *py_ckpt_save(PyObject *const *a, Py_ssize_t nargs) {  // x, out -> dat
   const at::Tensor out = ckpt_new(a[1], m, x, here);
   void *o = ckpt_ptr(out, m.rows, m.cols), *s = stream();
   CALL(dq_ckpt_save(&m.m, m.rows, m.cols, o, s));
-  return tuple({give(a[1], out), PyLong_FromLongLong(m.rows), PyLong_FromLongLong(m.cols)});
+  return tuple({wrote(a[1], out), PyLong_FromLongLong(m.rows), PyLong_FromLongLong(m.cols)});
 }
 PyObject *py_ckpt_load(PyObject *const *a, Py_ssize_t nargs) {  // data, rows, cols, bf16 (None: another type), out
   DQ_ARGS(5)
@@ -692,7 +697,7 @@ PyObject *py_ckpt_load(PyObject *const *a, Py_ssize_t nargs) {  // data, rows, c
   if (m.rows != c.rows || m.cols != c.cols) fail("out has another shape");
   void *i = ckpt_ptr(*c.data, c.rows, c.cols), *s = stream();
   CALL(dq_ckpt_load(i, c.rows, c.cols, &m.m, s));
-  return give(a[4], out);
+  return wrote(a[4], out);
 }
 PyObject *py_ckpt_weight_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, data, rows, cols, out, bias, bias_out, accumulate
   DQ_ARGS(8)
@@ -718,7 +723,7 @@ PyObject *py_ckpt_weight_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, da
   if (bytes) scratch = make_row((int64_t)bytes, at::kByte, dy);
   void *t = bytes ? scratch.data_ptr() : nullptr, *i = ckpt_ptr(*x.data, x.rows, x.cols), *s = stream();
   CALL(dq_ckpt_weight_grad(&g.m, i, g.rows, g.cols, x.cols, &w.m, d, accumulate, t, bytes, s));
-  return bias ? pair(give(a[4], out), give(a[6], db)) : give(a[4], out);
+  return bias ? pair(wrote(a[4], out), wrote(a[6], db)) : wrote(a[4], out);
 }
 at::ScalarType weight_type(const at::Tensor *weight, const at::Tensor *bias) {
   const at::Tensor *t = weight ? weight : bias;
@@ -752,8 +757,8 @@ PyObject *py_layer_norm(PyObject *const *a, Py_ssize_t nargs) {  // x, weight, b
   void *c = save ? ckpt.data_ptr() : nullptr, *s = stream();
   float *mu = save ? as<float>(mean.data_ptr()) : nullptr, *rs = save ? as<float>(rstd.data_ptr()) : nullptr;
   CALL(dq_layer_norm(&m.m, m.rows, m.cols, w, b, dtype_of(wt), (float)eps, &y.m, c, mu, rs, s));
-  if (!save) return give(a[5], out);
-  return tuple({give(a[5], out), wrap(ckpt), PyLong_FromLongLong(m.rows), PyLong_FromLongLong(m.cols), wrap(mean), wrap(rstd)});
+  if (!save) return wrote(a[5], out);
+  return tuple({wrote(a[5], out), wrap(ckpt), PyLong_FromLongLong(m.rows), PyLong_FromLongLong(m.cols), wrap(mean), wrap(rstd)});
 }
 PyObject *py_layer_norm_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, data, rows, cols, mean, rstd, weight, out, weight_out, bias_out, accumulate, bias
   DQ_ARGS(12)
@@ -791,7 +796,7 @@ PyObject *py_layer_norm_grad(PyObject *const *a, Py_ssize_t nargs) {  // dy, dat
   }
   void *c = ckpt_ptr(*x.data, x.rows, x.cols), *s = stream();
   CALL(dq_layer_norm_grad(&g.m, c, as<float>(mu), as<float>(rs), g.rows, g.cols, w, dtype_of(wt), &d.m, pw, pb, accumulate, t, bytes, s));
-  return tuple({give(a[7], out), weight ? give(a[8], dw) : none(), bias ? give(a[9], db) : none()});
+  return tuple({wrote(a[7], out), weight ? wrote(a[8], dw) : none(), bias ? wrote(a[9], db) : none()});
 }
 PyObject *py_gate(PyObject *const *a, Py_ssize_t nargs) {  // kind, z, u, save, out
   DQ_ARGS(5)
@@ -811,8 +816,8 @@ PyObject *py_gate(PyObject *const *a, Py_ssize_t nargs) {  // kind, z, u, save, 
   if (save && u) cu = ckpt_new(Py_None, m, z, here);
   void *pz = save ? cz.data_ptr() : nullptr, *pu = save && u ? cu.data_ptr() : nullptr, *s = stream();
   CALL(dq_gate(kind, &m.m, u ? &n.m : nullptr, m.rows, m.cols, &h.m, pz, pu, s));
-  if (!save) return give(a[4], out);
-  return tuple({give(a[4], out), PyLong_FromLongLong(m.rows), PyLong_FromLongLong(m.cols), wrap(cz), u ? wrap(cu) : none()});
+  if (!save) return wrote(a[4], out);
+  return tuple({wrote(a[4], out), PyLong_FromLongLong(m.rows), PyLong_FromLongLong(m.cols), wrap(cz), u ? wrap(cu) : none()});
 }
 PyObject *py_gate_grad(PyObject *const *a, Py_ssize_t nargs) {  // kind, dh, z's data, rows, cols, u's data, z_out, u_out
   DQ_ARGS(8)
@@ -838,7 +843,7 @@ PyObject *py_gate_grad(PyObject *const *a, Py_ssize_t nargs) {  // kind, dh, z's
   }
   void *pz = ckpt_ptr(*z.data, z.rows, z.cols), *pu = u ? ckpt_ptr(*u, z.rows, z.cols) : nullptr, *s = stream();
   CALL(dq_gate_grad(kind, &g.m, pz, pu, g.rows, g.cols, &mz.m, u ? &mu.m : nullptr, s));
-  return pair(give(a[6], dz), u ? give(a[7], du) : none());
+  return pair(wrote(a[6], dz), u ? wrote(a[7], du) : none());
 }
 PyObject *py_init(PyObject *const *a, Py_ssize_t nargs) {  // path of libdq.so, DqError
   DQ_ARGS(2)
