@@ -615,7 +615,10 @@ hipError_t run_norm_grad(const NormGrad &in, float *part, uint32_t parts, hipStr
 #define DQ_FITS(run, ...)                                                                                             \
   switch (k.group * 8 + k.keep) {                                                                                     \
     DQ_FIT(run, 16, 1, __VA_ARGS__) DQ_FIT(run, 32, 1, __VA_ARGS__)                                                   \
-    DQ_FIT(run, 64, 1, __VA_ARGS__) DQ_FIT(run, 64, 2, __VA_ARGS__) DQ_FIT(run, 64, 4, __VA_ARGS__)                   \
+    DQ_FIT(run, 64, 1, __VA_ARGS__) DQ_FIT(run, 64, 2, __VA_ARGS__)                                                   \
+    case 64 * 8 + 4:                                                                                                  \
+      if constexpr (__is_same(T, Bf16)) return past ? run<Fit<T, 64, 4, true>>(__VA_ARGS__) : run<Fit<T, 64, 4, false>>(__VA_ARGS__); \
+      break;                                                                                                          \
     case 128 * 8 + 2:                                                                                                 \
       if constexpr (__is_same(T, F32)) return past ? run<Fit<T, 128, 2, true>>(__VA_ARGS__) : run<Fit<T, 128, 2, false>>(__VA_ARGS__); \
       break;                                                                                                          \
