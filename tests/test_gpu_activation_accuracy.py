@@ -39,6 +39,17 @@ def test_gelu_left_of_zero(dev, lo, hi):
     assert mean_square(off) < 3.7 + 0.7 * lo * lo, mean_square(off)
 
 
+@pytest.mark.parametrize("lo,hi", [(-1.0, -0.1), (-0.1, 0.0), (0.0, 0.1), (0.1, 1.0)])
+def test_gelu_near_zero(dev, lo, hi):
+    """Phi = 0.5 + z Q(z^2): the fit and its coefficients 0.9 half steps of Q, its last addition 1, what is before counts a sixth, 0.4; the
+    addition of 0.5 one of Phi, the product with z one: at most."""
+    z = between(lo, hi, dev)
+    want = P.activation(z, "gelu")[0]
+    phi = want / z.double()
+    off = (B.dq_gate(z, kind="gelu").double() / want - 1).abs() / P.U
+    assert bool((off < 2.05 + 2.35 * (phi - 0.5).abs() / phi).all()), float(off.max())
+
+
 @pytest.mark.parametrize("lo,hi", [(-80.0, -40.0), (-40.0, -8.0), (-8.0, -1.0), (-1.0, 0.0), (0.0, 1.0), (1.0, 80.0)])
 def test_silu(dev, lo, hi):
     """z / (1 + e^-z): the exponential 1.42 half steps, the sum 1, the reciprocal 1.53, what the exponent's rounding is made up for with 1, the
