@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kMapThreads) void k_gate_grad(Walk8 w, Rows dh, Ckp
       float act, d;
       activation<T, KIND>(a.v[k], &act, &d);
       if constexpr (GATED) {
-        a.v[k] = g.v[k] * b.v[k] * d;
+        a.v[k] = g.v[k] * d * b.v[k];  // (dh u may be infinite where act' makes nothing of it)
         b.v[k] = g.v[k] * act;
       } else {
         a.v[k] = g.v[k] * d;

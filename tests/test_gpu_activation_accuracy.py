@@ -64,3 +64,14 @@ def test_silu_keeps_infinities_and_far_values(dev):
     z = torch.tensor([float("inf"), float("nan"), 3e38, 100.5, -100.5, -3e38, torch.finfo(torch.float32).min, 88.5, -104.0], device=dev)
     h = B.dq_gate(z, kind="silu")
     assert float(h[0]) == float("inf") and bool(torch.isnan(h[1])) and torch.equal(h[[2, 3, 7]], z[[2, 3, 7]]) and not h[[4, 5, 6, 8]].any()
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_large_gradients_where_the_derivative_is_zero(dev, dtype, kind):
+    """dz = dh act'(z) u with dh u past the largest number: zero where act'(z) is, infinite where it is one."""
+    one = torch.ones(2, 32, device=dev)
+    z = torch.tensor([[-224.0], [224.0]], device=dev) * one
+    _, saved = B.dq_gate(z.to(dtype), (one * 2.0 ** 70).to(dtype), kind, save=True)
+    dz, du = B.dq_gate_grad((one * 2.0 ** 70).to(dtype), saved)
+    assert bool((dz[0] == 0).all()) and bool((dz[1] == float("inf")).all()) and bool((du[0] == 0).all()) and bool((du[1] == 224 * 2.0 ** 70).all())
