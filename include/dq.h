@@ -157,7 +157,7 @@ dq_status dq_mx_decompress(dq_codec fmt, const void *packed_in, const void *loca
  * wider matrix is one), aligned to their entries, no more.  All matrices of a call have one type, except dw and what a load writes.
  * What a call writes must not overlap anything else it is given (DQ_EINVAL); two matrices side by side in a wider one do not
  * overlap (in one another's range, matrices of different ld count as overlapping).  rows or cols of zero: nothing is done, sums over
- * no rows are zero.  Sums and statistics are binary32, in an order that the sizes and types fix: the same call gives the same bits.
+ * no rows are zero (dq_ckpt_weight_grad with cols of zero refuses a db: DQ_EINVAL).  Sums and statistics are binary32, in an order that the sizes and types fix: the same call gives the same bits.
  * Infinities and NaN go where the formulas take them, with one exception (dq_ckpt_weight_grad). */
 typedef struct {
   void *data; /* device; read-only operands are not written */

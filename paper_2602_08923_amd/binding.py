@@ -318,7 +318,7 @@ def dq_ckpt_save(x, out=None):
 
 
 def dq_ckpt_load(ckpt, dtype=torch.float32, out=None):
-    """A checkpoint's values, [rows, cols] (exact in either type)."""
+    """A checkpoint's values, [rows, cols] (exact in either type), in dtype, or out's."""
     return _native().ckpt_load(*ckpt, dtype is torch.bfloat16 or (None if dtype is not torch.float32 else False), out)
 
 

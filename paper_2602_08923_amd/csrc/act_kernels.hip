@@ -3,7 +3,7 @@
 //
 // All are streams: every entry is read once and written once, a few dozen operations each, so memory bounds them.  Measured: a
 // checkpoint of bf16 16384 x 8192, saved and loaded, 134 us (6.1 TB/s), SiLU with a gate there, forward and backward, 351 us (6.1), GELU
-// at 16384 x 4096 125 us (5.4; with a gate 187, 5.8); rows off 16-byte borders up to 40 % more.
+// at 16384 x 4096 128 us (5.3; with a gate 177, 6.1); rows off 16-byte borders up to 40 % more.
 #include <atomic>
 #include <initializer_list>
 

@@ -230,7 +230,13 @@ inline Region region(const dq_matrix *m, uint64_t rows, uint64_t cols, bool writ
   return {m->data, rows, cols * e, rows > 1 ? m->ld * e : cols * e, written};
 }
 // Matrices of one call that together are larger than what the caches could keep of them go past the caches, where their rows lie on
-// 16-byte borders.
+// 16-byte borders.  What counts is a call and the one that reads what it wrote: us of both, 4096 columns, through the caches and past
+// them, the first call's inputs not in the caches:
+//   save and load       bf16 64 MiB a matrix 39, 37; 128 MiB 74, 67; 192 MiB 125, 102       fp32 64 MiB 33, 28; 100 MiB 50, 45; 128 MiB 62, 57
+//   gate, its gradient  bf16 32 MiB 48, 48; 48 MiB 67, 69; 64 MiB 99, 94; 100 MiB 166, 143  fp32 43, 42; 60, 62; 82, 81; 145, 125
+//   layer norm, its backward pass past them  bf16 32 MiB 43, 42; 64 MiB 69, 67               fp32 41, 37; 63, 58; its forward pass too: 72 and 64
+// With inputs that are still there, 64 MiB saved and loaded 34, 37; gates of 32 MiB 44, 48; the others are in the same order.  A single call
+// that is repeated on one input of 64 to 128 MiB takes up to a quarter less through the caches, which is not what a program does.
 constexpr uint64_t kPastBytes = 128ull << 20;
 inline bool on_16(const dq_matrix *m, uint64_t rows) { return (uintptr_t)m->data % 16 == 0 && (rows == 1 || m->ld * entry_bytes(m->dtype) % 16 == 0); }
 // Whether some written region meets another one.

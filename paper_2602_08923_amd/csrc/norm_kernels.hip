@@ -78,14 +78,15 @@ __device__ __forceinline__ void weights_at(const void *w, uint32_t bf16, uint64_
 // KEEP chunks of 8 entries each.  A row goes to one wave where that is enough (up to 2,048 entries) and there are rows for all, so that
 // its sums need no barrier; a wave has two or four of the short rows (up to 256 and 128 entries).  The next row is loaded while one
 // is worked on, and there are as many blocks as stay resident, so that most rows are loaded so.
-// Measured (forward and backward, 5.2 TB/s being a large copy's rate): bf16 16384 x 2048 69 us (4.9 TB/s), 200000 x 128 57 us (4.5),
-// 65536 x 2048 228 us (5.9), 16384 x 4096 129 us (5.2), 4096 x 16384 159 us (4.2); fp32 16384 x 4096 207 us (5.8), 1021 x 6151 37 us (3.1).
+// Measured (forward and backward, 5.2 TB/s being a large copy's rate): bf16 16384 x 2048 68 to 73 us (4.6 to 5.0 TB/s), 200000 x 128 53
+// (4.9), 65536 x 2048 224 (6.0), 16384 x 4096 128 (5.3), 4096 x 16384 152 (4.5); fp32 16384 x 4096 208 (5.8), 8192 x 8192 216 (5.6), 4096 x
+// 16384 233 (5.2), 65536 x 500 135 (4.4), 1021 x 6151 38 (3.0).
 //
 // PAST: rows of large calls go past the caches.  A wave's loads and stores then have to cover memory without gaps, so a chunk is 16 bytes,
 // twice as many of 4 entries in fp32.  Forward and backward, through the caches and past them: bf16 65536 x 2048 265 and 228 us,
 // 16384 x 4096 136 and 128, fp32 16384 x 4096 231 and 207.  Below, chunks of 8 are as good or better (fp32 1024 x 8192 41 and 43), and
 // better over odd rows (fp32 3000 x 7001 96, 105 with 4).  Both add a row up in the same order (see RowSums).  The forward pass takes twice
-// the size for large (bf16 16384 x 2048 by itself 21.9 and 24.3 us: the matrix that it reads may still be in the caches).
+// the size for large (see kPastBytes: 128 MiB of x and y in bf16, with the backward pass, 67 us, 72 if it went past the caches too).
 //
 // A block's groups take a row each, the block then the next rows; all of them come round as often as each other.
 template <typename T, uint32_t GROUP, uint32_t KEEP, bool PAST>
@@ -572,11 +573,13 @@ constexpr uint32_t kRowBlocks = 512;  // blocks that longer rows are dealt to
 uint32_t row_blocks(uint64_t rows) { return (uint32_t)(rows < kRowBlocks ? rows : kRowBlocks); }
 
 // How rows are kept: threads to a row and chunks to a thread (group 0: the row is too long).  Measured, forward and backward:
-// (through the caches) 16384 x 2056 in bf16 takes 89 us by groups of 128, 116 by 256; 4096 x 16384 169 us by groups of 512 that load ahead, 185 by 1,024 that
-// have no registers for it; 200000 x 128 59 us by groups of 16, 150 by 64.  Few rows are shared by more threads: the two kernels take 6
-// and 11 us for 1024 x 2048 by groups of 64, 6 and 7 by 256 (256 rows: 5 and 10, 4 and 4; 3000: 10 and 15, 11 and 12; 6000: 14 and 18, 17
-// and 19), for 2000 x 1024 5 and 7 by 64, 7 and 8 by 256.  Rows of 1,025 to 2,048 entries: bf16 8192 x 2048 42 us by 64, 43 by 128 (8192 x
-// 2047 48 and 57); fp32, whose next row takes twice the registers, 72 by 64 (the backward pass then spills), 63 by 128.
+// (through the caches) 16384 x 2056 in bf16 takes 89 us by groups of 128, 116 by 256; 4096 x 16384 169 us by groups of 512 that load ahead,
+// 185 by 1,024 that have no registers for it; 200000 x 128 59 us by groups of 16, 150 by 64.  Few rows are shared by more threads: the two
+// kernels take 6 and 11 us for 1024 x 2048 by groups of 64, 6 and 7 by 256 (256 rows: 5 and 10, 4 and 4; 3000: 10 and 15, 11 and 12; 6000: 14
+// and 18, 17 and 19), for 2000 x 1024 5 and 7 by 64, 7 and 8 by 256.  Rows of 1,025 to 2,048 entries: bf16 8192 x 2048 42 us by 64, 43 by 128
+// (8192 x 2047 48 and 57); fp32, whose next row takes twice the registers, 72 by 64 (the backward pass then spills), 63 by 128.  Rows of 2,049 to
+// 3,072, the two calls by 128 and by 256: bf16 1000 x 3000 8 and 14, 8 and 14; 2048 rows 11 and 16, 13 and 17; 3000 13 and 18, 15 and 21; 8000 24 and 33,
+// 26 and 40; fp32 1000 10 and 15, 9 and 15; 2048 14 and 19, 13 and 20; 4000 20 and 28, 21 and 29; 8000 39 and 49, 39 and 54.
 struct Kept {
   uint32_t group, keep;
 };
@@ -592,12 +595,16 @@ Kept kept(uint64_t rows, uint64_t cols, bool f32) {
   if ((uint64_t)group * keep < chunks) group = 0;
   return {group, keep};
 }
-// Parts of the sums over rows: blocks of the backward pass (Fit::kGroups rows at a time), or slices of the rows.
+// Parts of the sums over rows: blocks of the backward pass (Fit::kGroups rows at a time), or slices of the rows.  256, an MI355X's CUs, whatever the
+// device has: the sums' order and the scratch memory follow from sizes alone.
 uint32_t norm_parts(uint64_t rows, uint64_t cols) {
   const Kept k = kept(rows, cols, false);  // (fp32 differs only where there are rows enough for 256 parts either way)
   const uint64_t at_once = k.group == 0 ? 8 : k.group < 512 ? 512 / k.group : 1, parts = (rows + at_once - 1) / at_once;
   return (uint32_t)(parts < 256 ? parts : 256);
 }
+// As many blocks as an MI355X keeps by their registers.  One block more to a CU, and one fewer: forward pass, fp32 8192 x 8192 (two to a CU) 119
+// and 147 us, 108 as it is; 16384 x 3000 (three) 94 and 88, 88; bf16 50 and 56, 49; 8192 x 6000 (three) 49 and 55, 49; 100000 x 512 (four; eight
+// for more) 52 and 55, 52; 4096 x 16384 (one; two for more) 75, 75.
 template <typename F>
 hipError_t run_norm(const NormIn &in, const Rows &y, const CkptOut &saved, float *mean, float *rstd, hipStream_t s) {
   constexpr uint32_t kBlock = F::kGroup < 256 ? 256 : F::kGroup, kGroups = kBlock / F::kGroup;

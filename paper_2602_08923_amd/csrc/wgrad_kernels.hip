@@ -129,7 +129,7 @@ struct Stage {
 // A block's walk over the tokens, one tile at a time.  Steps go through two buffers in LDS: while the matrix cores read one, the next
 // step's operands go to the other, from registers.  SMALL: fewer than 8 outs, loaded entry by entry.
 //
-// Tiles of 256 x 256 by 8 waves: bf16 16384 x 8192 x 2048 in 436 to 470 us by the card (1.17 to 1.26 PFLOP/s; the library's best large
+// Tiles of 256 x 256 by 8 waves: bf16 16384 x 8192 x 2048 in 434 to 486 us by the card (1.13 to 1.27 PFLOP/s; the library's best large
 // product, 1.34), the matrix cores busy 68 % of the cycles at a clock of 1.74 GHz: power bounds it.  Four waves of 128 x 128 took 514
 // us; x written to LDS without bank conflicts, by lanes that swap their halves, 4 % more (the selections cost more than the conflicts);
 // waves of raised priority around the products 3 % more.  fp32 4096 x 8192 x 8192: 1,220 us, three products each (1.35 PFLOP/s).
@@ -519,8 +519,10 @@ constexpr uint32_t kEdges[3] = {64, 128, 256}, kToks[2][3] = {{32, 32, 32}, {64,
 constexpr uint32_t kManySplits = 16;  // of which several threads join one sum (30000 x 64 x 64, a hundred splits: 10 us; 40 by one thread a sum)
 
 // The cut that costs least, by what was measured (MI355X, microseconds): a step of a block alone on its CU and of one among as many as
-// fit, the launch, the tiles' way to memory, and what splits add, a launch and their sums' way to memory and back at 5 TB/s.  Large tiles read and move
-// least for what they multiply; small ones and splits give every CU a part where sums are few.
+// fit, the launch, the tiles' way to memory, and what splits add, a launch and their sums' way to memory and back at 5 TB/s.  Large tiles
+// read and move least for what they multiply; small ones and splits give every CU a part where sums are few.  Over 16 sizes in each type
+// the choice is within 10 % of the best tile and split, but for fp32 65537 x 200 x 136 (34 to 39 us, 33 with 128 x 128).  256 CUs whatever the
+// device has: the order of sums and the scratch memory follow from sizes and types alone.
 Cut cut_of(dq_dtype dtype, uint64_t rows, uint64_t outs, uint64_t cols) {
   constexpr uint64_t kCus = 256;
   struct Cost { uint32_t fit; double alone, among, tile; };  // blocks on a CU, a step's time, their tiles' way to memory
