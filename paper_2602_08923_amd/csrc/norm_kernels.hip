@@ -577,9 +577,9 @@ uint32_t row_blocks(uint64_t rows) { return (uint32_t)(rows < kRowBlocks ? rows 
 // 185 by 1,024 that have no registers for it; 200000 x 128 59 us by groups of 16, 150 by 64.  Few rows are shared by more threads: the two
 // kernels take 6 and 11 us for 1024 x 2048 by groups of 64, 6 and 7 by 256 (256 rows: 5 and 10, 4 and 4; 3000: 10 and 15, 11 and 12; 6000: 14
 // and 18, 17 and 19), for 2000 x 1024 5 and 7 by 64, 7 and 8 by 256.  Rows of 1,025 to 2,048 entries: bf16 8192 x 2048 42 us by 64, 43 by 128
-// (8192 x 2047 48 and 57); fp32, whose next row takes twice the registers, 72 by 64 (the backward pass then spills), 63 by 128.  Rows of 2,049 to
-// 3,072, the two calls by 128 and by 256: bf16 1000 x 3000 8 and 14, 8 and 14; 2048 rows 11 and 16, 13 and 17; 3000 13 and 18, 15 and 21; 8000 24 and 33,
-// 26 and 40; fp32 1000 10 and 15, 9 and 15; 2048 14 and 19, 13 and 20; 4000 20 and 28, 21 and 29; 8000 39 and 49, 39 and 54.
+// (8192 x 2047 48 and 57); fp32, whose next row takes twice the registers, 72 by 64 (the backward pass then spills), 63 by 128.  Longer rows that
+// three chunks of 128 threads hold, the two calls by 128 and by 256: bf16 1000 x 3000 8 and 14, 8 and 14; 2048 rows 11 and 16, 13 and 17; 3000 13 and 18,
+// 15 and 21; 8000 24 and 33, 26 and 40; fp32 1000 10 and 15, 9 and 15; 2048 14 and 19, 13 and 20; 4000 20 and 28, 21 and 29; 8000 39 and 49, 39 and 54.
 struct Kept {
   uint32_t group, keep;
 };
